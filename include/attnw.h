@@ -122,6 +122,100 @@ int attnw_project_qk(const void* X, const void* Wq, const void* Wk, void* Q, voi
                      int d, void* stream);
 
 /*
+ * Rotary positions.  A pair of features (a, b) of a row at position n turns by the angle n f, f the pair's frequency:
+ *     a' = amplitude (a cos(n f) - b sin(n f)),   b' = amplitude (b cos(n f) + a sin(n f));
+ * features from `rotary` on are copied.  `inverse` != 0 turns by -n f, with the same amplitude: the transpose, which takes the
+ * gradient of the result to the gradient of X.
+ *
+ *   X, Y         device, bfloat16 (attnw_rope) or float32 (attnw_rope_f32), [B, H, N, d] with the strides given: x_strides[3], y_strides[3], HOST
+ *                arrays, in elements, of the first three dimensions; rows of d are contiguous and begin on 16-byte boundaries.  Y may be X with the
+ *                same strides (in place); any other overlap is refused.  A dimension of X may be broadcast (stride 0), none of Y.
+ *   positions    device, int32, [B, N]; any value
+ *   frequencies  device, float64, [rotary / 2], radians a position; may be NULL where rotary is 0
+ *   B,H,N        >= 1, H <= 65535;  d in {64, 128};  rotary a multiple of 16 (else ATTNW_ERR_UNSUPPORTED), 0 ... d
+ *   layout       0: pairs (c, c + rotary / 2);  1: pairs (2c, 2c + 1)
+ *   amplitude    finite (1 unless the scaling of the frequencies asks for more)
+ * Angles are computed in float64, the rotation in float32; the result is rounded once.
+ */
+int attnw_rope(const void* X, const int* positions, const double* frequencies, void* Y, int B, int H, int N, int d, int rotary,
+               const long long* x_strides, const long long* y_strides, int layout, int inverse, float amplitude, void* stream);
+int attnw_rope_f32(const void* X, const int* positions, const double* frequencies, void* Y, int B, int H, int N, int d, int rotary,
+                   const long long* x_strides, const long long* y_strides, int layout, int inverse, float amplitude, void* stream);
+
+/*
+ * A paged cache of keys and values.  The keys of sequence b are those of the pages that row b of `table` names, page by page in order.
+ *
+ *   K, V         device, bfloat16, [pages, kv_heads, page, d]
+ *   table        device, int32, [sequences, table_width]; entries behind a sequence's length are not looked at
+ *   lengths      device, int32, [sequences]: keys of each sequence, for attnw_cache_append and attn_paged with the new tokens included
+ *   page         a power of two from 16 to 1024 (else ATTNW_ERR_UNSUPPORTED);  d in {64, 128}
+ *   pages, kv_heads, sequences, table_width  >= 1;  sequences * kv_heads <= 65535;  table_width * page <= 2^28
+ * The table, the lengths and the starts of the calls below are read on the device only, and none of their values leads out of bounds: a length
+ * counts as at least 0 and at most table_width * page; a page outside the cache is not written, and reads as zeros.  Two entries that
+ * name one page share its keys; calls that write such a page give unspecified values there.
+ * New tokens of all sequences lie one behind the other: those of sequence b are starts[b] ... starts[b + 1] - 1 (device, int32,
+ * [sequences + 1], ascending), and are the last ones of their sequence: token t has place lengths[b] - (starts[b + 1] - t).  Tokens in
+ * front of starts[0] and from starts[sequences] on belong to nobody: nothing is written for them.
+ */
+typedef struct attnw_cache {
+    void* K;
+    void* V;
+    const int* table;
+    const int* lengths;
+    int pages, kv_heads, page, d, sequences, table_width;
+} attnw_cache;
+
+/*
+ * attnw_cache_append: the new tokens' queries and keys turned by their positions (attnw_rope), keys and values written to their places.
+ * One launch.
+ *
+ *   Q, Q_out     device, bfloat16, [tokens, heads, d], both NULL where only the cache is written; Q_out may be Q with the same strides
+ *   K, V         device, bfloat16, [tokens, kv_heads, d]
+ *   strides      HOST, 8 values in elements: token and head strides of Q, K, V and Q_out (as for attnw_rope)
+ *   positions    device, int32, [tokens];  frequencies  device, float64, [rotary / 2].  Both may be NULL where rotary is 0: nothing turns
+ * Q_out, the caches and the other operands must not overlap (columns of one array of tokens do not).  A token whose place is negative, which
+ * has more new tokens behind it than its sequence's length, is not written to the cache.
+ */
+int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, const void* V, void* Q_out, const long long* strides, const int* starts,
+                       const int* positions, const double* frequencies, int tokens, int heads, int rotary, int layout, float amplitude, void* stream);
+
+/*
+ * attn_paged: attention of the new tokens over their sequences' keys, each over those up to its own place:
+ *   O[t,h] = sum_j p_j V[j],  p_j = exp(z_j - lse[t,h]),  z_j = scale * Q[t,h] . K[j],  lse[t,h] = log sum_j exp(z_j),
+ * with the keys of key head h / (heads / kv_heads).  A token that sees no key has O = 0 and lse = -infinity.
+ *
+ *   Q            device, bfloat16, [tokens, heads, d]; q_strides: HOST, token and head stride in elements (not 0)
+ *   O            device, bfloat16, [tokens, heads, d], contiguous
+ *   lse          device, float32, [tokens, heads], or NULL
+ *   mass, mass_out  device, float32, [sequences, kv_heads, table_width * page], or both NULL: mass_out[b,g,j] = mass[b,g,j] + the sum of
+ *                the weights p_j that the key receives from the new tokens and the heads of its group; mass_out may be mass
+ *   workspace    device, 16-byte aligned, at least attn_paged_workspace(cache, tokens, heads, mass != NULL) bytes, in use until the
+ *                call's work has ended; it keeps nothing from one call to the next and may hold anything
+ *   heads        a multiple of kv_heads, at most 128 to one;  scale finite, >= 0;  tokens * heads < 2^29
+ * Keys behind a sequence's length are never part of a result, whatever the cache holds there.
+ */
+int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
+               float* mass_out, void* workspace, long long workspace_bytes, int tokens, int heads, float scale, void* stream);
+long long attn_paged_workspace(const attnw_cache* cache, int tokens, int heads, int weigh);
+
+/*
+ * attnw_cache_evict: shortens the sequences that are longer than `budget`.  Of such a sequence each key head keeps its last `recent` keys and,
+ * of the others, the budget - recent of most weight `mass` (of equal ones the first; NaN counts as less than any number); keys, values and weights
+ * that stay move to the sequence's first `budget` places, in their order.  Sequences of at most `budget` keys stay whole.
+ *
+ *   mass         device, float32, [sequences, kv_heads, table_width * page]: what attn_paged adds up
+ *   table_out    device, int32, [sequences, table_out_width]: the pages that take what stays, none of which the cache's table names; NULL (or the
+ *                cache's table itself, of the same width): in place
+ *   mass_out     device, float32, [sequences, kv_heads, table_out_width * page] (in place: table_width); zero behind the keys that
+ *                stay; may be mass where the sizes agree
+ *   kept         device, int32, [sequences, kv_heads, budget]: the old place of each key that stays, -1 behind them
+ *   lengths_out  device, int32, [sequences]: the new lengths; not cache->lengths
+ *   budget       1 ... the places of the pages that take them;  recent 0 ... budget
+ */
+int attnw_cache_evict(const attnw_cache* cache, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out,
+                      int budget, int recent, void* stream);
+
+/*
  * Which kernel attn_fused uses (process-wide; the results agree within the stated tolerance):
  *   0  default: the one-pass kernel
  *   1  two-pass kernel: row maxima and sums in a first pass over the keys, normalised weights times V in a second

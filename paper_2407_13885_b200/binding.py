@@ -8,6 +8,7 @@ for device memory and streams only (``tensor.data_ptr()``, ``torch.cuda.current_
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -15,6 +16,12 @@ import torch
 from . import build as _build
 
 _vp, _int, _ll, _float = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float
+
+class Cache(ctypes.Structure):
+    """``attnw_cache`` of include/attnw.h."""
+    _fields_ = [("K", _vp), ("V", _vp), ("table", _vp), ("lengths", _vp), ("pages", _int), ("kv_heads", _int), ("page", _int), ("d", _int),
+                ("sequences", _int), ("table_width", _int)]
+
 
 # name -> (restype, argtypes); mirrors include/attnw.h one to one
 SIGNATURES = {
@@ -28,6 +35,12 @@ SIGNATURES = {
     "softmax_rows_host": (_int, [_vp, _vp, _ll, _ll, _int]),
     "attnw_host_release": (_int, []),
     "attnw_fused_noalloc": (_int, [_vp, _vp, _vp, _int, _int, _int, _int, ctypes.c_float, _vp]),
+    "attnw_rope": (_int, [_vp, _vp, _vp, _vp, _int, _int, _int, _int, _int, _vp, _vp, _int, _int, _float, _vp]),
+    "attnw_rope_f32": (_int, [_vp, _vp, _vp, _vp, _int, _int, _int, _int, _int, _vp, _vp, _int, _int, _float, _vp]),
+    "attnw_cache_append": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _int, _int, _int, _float, _vp]),
+    "attn_paged": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _ll, _int, _int, _float, _vp]),
+    "attn_paged_workspace": (_ll, [_vp, _int, _int, _int]),
+    "attnw_cache_evict": (_int, [_vp, _vp, _int, _vp, _vp, _vp, _vp, _int, _int, _vp]),
     "attnw_query_status": (_int, [_vp, ctypes.POINTER(ctypes.c_uint)]),
     "attnw_selftest_wait_timeout": (_int, [_ll, _vp]),
     "attnw_selftest_exchange_tags": (_int, [ctypes.c_uint, _vp]),
@@ -173,6 +186,83 @@ def softmax_rows(S: torch.Tensor, P: torch.Tensor | None = None, out_dtype: torc
                  stream=None) -> torch.Tensor:
     """Row-wise Softmax of float32 scores ``S [rows, cols]`` -> ``P`` (bfloat16 or float32)."""
     return _native.softmax_rows(S, P, out_dtype, None if stream is None else _stream_ptr(stream))
+
+
+def rope_frequencies(rotary: int, base: float = 10000.0, *, scaling: str | None = None, factor: float = 1.0, original: int | None = None,
+                     low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """Frequencies of the pairs of ``rotary`` features for ``rope`` and ``cache_append``: ``base ** (-2 i / rotary)``, float64 on the CPU.
+
+    ``scaling`` stretches them to contexts ``factor`` times as long as those a model was trained on:
+
+    * ``"linear"``: every frequency divided by ``factor`` (positions squeezed together);
+    * ``"base"``: a larger base, ``base * factor ** (rotary / (rotary - 2))``, so that the fastest pair stays and the slowest is divided by ``factor``;
+    * ``"by_parts"``: pairs that turn at least ``high`` times within the ``original`` context stay, those that turn at most ``low``
+      times are divided by ``factor``, the others lie in between, by their number of turns."""
+    if rotary < 0 or rotary % 2:
+        raise ValueError("rotary must be even and not negative")
+    if not (math.isfinite(base) and base > 0 and math.isfinite(factor) and factor > 0):
+        raise ValueError("base and factor must be positive")
+    if scaling not in (None, "linear", "base", "by_parts"):
+        raise ValueError("scaling must be None, \"linear\", \"base\" or \"by_parts\"")
+    if scaling == "base":
+        if rotary < 4:
+            raise ValueError("scaling \"base\" needs at least two pairs")
+        base = base * factor ** (rotary / (rotary - 2))
+    f = base ** (torch.arange(0, rotary, 2, dtype=torch.float64) / -max(rotary, 1))
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_parts":
+        if original is None or original < 1 or not low < high:
+            raise ValueError("scaling \"by_parts\" needs the original context and low < high")
+        stays = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = f * stays + f / factor * (1.0 - stays)
+    return f
+
+
+def rope(X: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, *, layout: str = "half", amplitude: float = 1.0,
+         inverse: bool = False, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Rotary positions of ``X [B, H, N, d]`` (CUDA, bfloat16 or float32, d contiguous, the other strides any): the first
+    ``2 * len(frequencies)`` features of each row turn, in pairs, by ``positions[b, n] * frequencies`` (int32 ``[B, N]``, float64).
+
+    ``layout``: "half" pairs feature c with c + rotary / 2, "interleaved" 2c with 2c + 1.  ``inverse=True`` turns back: the gradient of
+    the result gives that of ``X``.  ``out`` may be ``X`` (in place) or have other strides, e.g. token-major memory for ``cache_append`` and
+    ``attn_paged``.  Asynchronous on ``stream`` (default: torch's current stream)."""
+    return _native.rope(X, positions, frequencies, layout, amplitude, inverse, out, None if stream is None else _stream_ptr(stream))
+
+
+def cache_append(Q: torch.Tensor | None, K: torch.Tensor, V: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, table: torch.Tensor,
+                 lengths: torch.Tensor, starts: torch.Tensor, positions: torch.Tensor | None = None, frequencies: torch.Tensor | None = None, *,
+                 layout: str = "half", amplitude: float = 1.0, Q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """New tokens into a paged cache: ``Q [tokens, heads, d]`` and ``K [tokens, kv_heads, d]`` turned as by ``rope`` (unless there are no
+    ``positions``), keys and values ``V`` written to their places in ``K_cache, V_cache [pages, kv_heads, page, d]``.  Returns the turned queries
+    (None without ``Q``).
+
+    ``table [sequences, width]``, ``lengths [sequences]`` (new tokens included) and ``starts [sequences + 1]`` (of each sequence's new tokens) are
+    int32 on the GPU; see ``attnw_cache`` in include/attnw.h.  Asynchronous on ``stream``."""
+    return _native.cache_append(K_cache, V_cache, table, lengths, starts, Q, K, V, positions, frequencies, layout, amplitude, Q_out,
+                                None if stream is None else _stream_ptr(stream))
+
+
+def attn_paged(Q: torch.Tensor, K_cache: torch.Tensor, V_cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor,
+               scale: float, *, O: torch.Tensor | None = None, lse: torch.Tensor | None = None, mass: torch.Tensor | None = None,
+               mass_out: torch.Tensor | None = None, stream=None):
+    """Attention of new tokens ``Q [tokens, heads, d]`` over a paged cache, each over its sequence's keys up to its own place.  Returns
+    ``O [tokens, heads, d]``; with ``mass [sequences, kv_heads, width * page]`` (float32) ``(O, mass_out)``, ``mass`` plus the weights that each key
+    received (``mass_out=mass``: in place).  ``lse``: a float32 ``[tokens, heads]`` that takes the logarithms of the sums.
+
+    The cache and its index tensors as for ``cache_append``.  Scratch memory is torch's, on the call's stream.  Asynchronous on ``stream``."""
+    return _native.attn_paged(K_cache, V_cache, table, lengths, starts, Q, scale, O, lse, mass, mass_out, None if stream is None else _stream_ptr(stream))
+
+
+def cache_evict(K_cache: torch.Tensor, V_cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, mass: torch.Tensor, budget: int, recent: int, *,
+                table_out: torch.Tensor | None = None, mass_out: torch.Tensor | None = None,
+                stream=None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Shortens the sequences of a paged cache that are longer than ``budget`` to it: each key head keeps its last ``recent`` keys and the others of
+    most ``mass`` (of equal ones the first), moved together in their order - in place, or into the pages of ``table_out``, which must be others.
+    Returns ``(kept, lengths, mass)``: the old places of the keys that stay (int32 ``[sequences, kv_heads, budget]``, -1 behind them), the new
+    lengths and the weights in their new places.  Asynchronous on ``stream``."""
+    return _native.cache_evict(K_cache, V_cache, table, lengths, mass, budget, recent, table_out, mass_out,
+                               None if stream is None else _stream_ptr(stream))
 
 
 def _require_host(t: torch.Tensor, name: str, dtype) -> None:

@@ -1,5 +1,6 @@
 // C ABI of libattnw.so: argument validation, tensor-map encoding and kernel launches.
 // The contract of every entry point is stated in include/attnw.h.
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -22,6 +23,9 @@
 #include "attnw_gridrow.cuh"
 #include "softmax_rows.cuh"
 #include "softmax_rows_smem.cuh"
+#include "rope.cuh"
+#include "cache_evict.cuh"
+#include "attn_paged_simple.cuh"
 
 namespace {
 
@@ -1135,6 +1139,8 @@ int launch_gridrow_noalloc(DeviceInfo* dev, NoAllocState* st, const void* Q, con
 
 }  // namespace
 
+#include "cache_calls.cuh"
+
 extern "C" {
 
 int attn_fused(const void* Q, const void* K, const void* V, void* O, int B, int H, int N, int d, float scale,
@@ -1163,6 +1169,37 @@ int attnw_project_qk(const void* X, const void* Wq, const void* Wk, void* Q, voi
     rc = load_encoder();
     if (rc != ATTNW_OK) return rc;
     return launch_project(dev, X, Wq, Wk, Q, K, B, N, d_model, H, d, static_cast<cudaStream_t>(stream));
+}
+
+int attnw_rope(const void* X, const int* positions, const double* frequencies, void* Y, int B, int H, int N, int d, int rotary, const long long* x_strides,
+               const long long* y_strides, int layout, int inverse, float amplitude, void* stream) {
+    return rope_entry<__nv_bfloat16>(X, positions, frequencies, Y, B, H, N, d, rotary, x_strides, y_strides, layout, inverse, amplitude, stream);
+}
+
+int attnw_rope_f32(const void* X, const int* positions, const double* frequencies, void* Y, int B, int H, int N, int d, int rotary,
+                   const long long* x_strides, const long long* y_strides, int layout, int inverse, float amplitude, void* stream) {
+    return rope_entry<float>(X, positions, frequencies, Y, B, H, N, d, rotary, x_strides, y_strides, layout, inverse, amplitude, stream);
+}
+
+int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, const void* V, void* Q_out, const long long* strides, const int* starts,
+                       const int* positions, const double* frequencies, int tokens, int heads, int rotary, int layout, float amplitude, void* stream) {
+    return append_entry(cache, Q, K, V, Q_out, strides, starts, positions, frequencies, tokens, heads, rotary, layout, amplitude, stream);
+}
+
+long long attn_paged_workspace(const attnw_cache* cache, int tokens, int heads, int weigh) {
+    if (!cache || tokens < 1 || heads < 1) return 0;
+    return static_cast<long long>(paged_workspace(cache, tokens, heads, weigh != 0, false).bytes);
+}
+
+int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
+               float* mass_out, void* workspace, long long workspace_bytes, int tokens, int heads, float scale, void* stream) {
+    return paged_entry(cache, Q, q_strides, starts, O, lse, mass, mass_out, workspace, workspace_bytes < 0 ? 0ull : static_cast<unsigned long long>(workspace_bytes),
+                       tokens, heads, scale, stream);
+}
+
+int attnw_cache_evict(const attnw_cache* cache, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out,
+                      int budget, int recent, void* stream) {
+    return evict_entry(cache, table_out, table_out_width, mass, mass_out, kept, lengths_out, budget, recent, stream);
 }
 
 int attnw_set_rows_variant(int variant) {

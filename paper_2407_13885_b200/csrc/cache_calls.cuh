@@ -1,0 +1,309 @@
+// Checks and launches of the calls around a paged cache (attnw_rope, attnw_cache_append, attn_paged, attnw_cache_evict).  Part of
+// attnw_api.cu, whose helpers it uses.
+#pragma once
+
+namespace {
+
+// Where a strided [n0, n1, n2, row] array lies: its bytes from `p` on, and the largest stride's period.  Strides in elements, as many
+// dimensions as sizes; a dimension of size 1 has no say.
+struct Extent {
+    uintptr_t begin = 0, end = 0;
+    unsigned long long pitch = 0;  // bytes from one token (the dimension `by`) to the next, 0 if there is one token
+    unsigned long long inner = 0;  // bytes that the rows of one token, or of tokens whole pitches apart, cover of a pitch
+};
+
+// Strides of a kernel's operand: not negative, and rows on 16-byte boundaries.  No dimension with more than one index may be
+// broadcast where `written`.  Returns an attnw_status.
+int check_strides(const long long* strides, const long long* sizes, int n, int esize, bool written) {
+    for (int i = 0; i < n; ++i) {
+        if (sizes[i] <= 1) continue;
+        if (strides[i] < 0 || strides[i] > (1ll << 40)) return ATTNW_ERR_BAD_SHAPE;
+        if (strides[i] * esize % 16 != 0) return ATTNW_ERR_MISALIGNED;
+        if (written && strides[i] == 0) return ATTNW_ERR_BAD_SHAPE;
+    }
+    return ATTNW_OK;
+}
+
+// `sizes` and `strides` of [.., token, .., d] without d; `token` is the index of the dimension whose rows lie side by side.
+Extent extent_of(const void* p, const long long* strides, const long long* sizes, int n, int token, long long d, int esize) {
+    Extent e;
+    unsigned long long all = static_cast<unsigned long long>(d) * esize, inner = all;
+    for (int i = 0; i < n; ++i) {
+        const unsigned long long span = sizes[i] > 1 ? static_cast<unsigned long long>(sizes[i] - 1) * strides[i] * esize : 0;
+        all += span;
+        const bool whole_pitches = sizes[token] > 1 && strides[token] > 0 && strides[i] % strides[token] == 0;
+        if (i != token && !whole_pitches) inner += span;
+    }
+    e.begin = reinterpret_cast<uintptr_t>(p);
+    e.end = e.begin + all;
+    e.pitch = sizes[token] > 1 ? static_cast<unsigned long long>(strides[token]) * esize : 0;
+    e.inner = inner;
+    return e;
+}
+
+// May the two share a byte?  Operands cut out of one array of tokens (queries, keys and values side by side) do not where their columns
+// differ, although their extents cross.
+bool may_overlap(const Extent& a, const Extent& b) {
+    if (a.end <= b.begin || b.end <= a.begin) return false;
+    if (a.pitch == 0 || a.pitch != b.pitch || a.inner > a.pitch || b.inner > a.pitch) return true;
+    const unsigned long long at = (b.begin >= a.begin ? b.begin - a.begin : a.pitch - (a.begin - b.begin) % a.pitch) % a.pitch;
+    return at < a.inner || at + b.inner > a.pitch;
+}
+
+int check_turn(const void* frequencies, int rotary, int d, int layout, float amplitude) {
+    if (layout != 0 && layout != 1) return ATTNW_ERR_BAD_SHAPE;
+    if (!std::isfinite(amplitude)) return ATTNW_ERR_BAD_SHAPE;
+    if (rotary < 0 || rotary > d) return ATTNW_ERR_BAD_SHAPE;
+    if (rotary % 16 != 0) return ATTNW_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(frequencies) % 8 != 0) return ATTNW_ERR_MISALIGNED;
+    return ATTNW_OK;
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Heads that one thread walks with its cosines and sines: all of them where the tokens alone fill the device (1024 threads an SM), fewer
+// otherwise, since latency is what a small call spends its time on.
+int heads_each(long long threads, int heads, int sm_count) {
+    const long long groups = std::max(1ll, static_cast<long long>(sm_count) * 1024 / std::max(1ll, threads));
+    return static_cast<int>((heads + groups - 1) / groups);
+}
+
+template <typename T>
+int rope_entry(const void* X, const int* positions, const double* frequencies, void* Y, int B, int H, int N, int d, int rotary,
+               const long long* x_strides, const long long* y_strides, int layout, int inverse, float amplitude, void* stream) {
+    if (!X || !positions || (rotary > 0 && !frequencies) || !Y || !x_strides || !y_strides) return ATTNW_ERR_NULL_POINTER;
+    if (B < 1 || H < 1 || N < 1 || d < 1 || H > 65535) return ATTNW_ERR_BAD_SHAPE;
+    if (d != 64 && d != 128) return ATTNW_ERR_UNSUPPORTED;
+    int rc = check_turn(frequencies, rotary, d, layout, amplitude);
+    if (rc != ATTNW_OK) return rc;
+    const long long sizes[3] = {B, H, N};
+    rc = check_strides(x_strides, sizes, 3, sizeof(T), false);
+    if (rc == ATTNW_OK) rc = check_strides(y_strides, sizes, 3, sizeof(T), true);
+    if (rc != ATTNW_OK) return rc;
+    if (!aligned16(X) || !aligned16(Y) || !aligned4(positions)) return ATTNW_ERR_MISALIGNED;
+    const Extent x = extent_of(X, x_strides, sizes, 3, 2, d, sizeof(T)), y = extent_of(Y, y_strides, sizes, 3, 2, d, sizeof(T));
+    bool in_place = X == Y;
+    for (int i = 0; i < 3; ++i) in_place = in_place && (sizes[i] == 1 || x_strides[i] == y_strides[i]);
+    if (!in_place && may_overlap(x, y)) return ATTNW_ERR_ALIASING;
+    const unsigned long long tokens = static_cast<unsigned long long>(B) * N;
+    const Extent index[2] = {extent_of(positions, sizes, sizes, 0, 0, static_cast<long long>(tokens), 4), extent_of(frequencies, sizes, sizes, 0, 0, rotary / 2, 8)};
+    for (const Extent& e : index)
+        if (y.begin < e.end && e.begin < y.end) return ATTNW_ERR_ALIASING;
+    DeviceInfo* dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != ATTNW_OK) return rc;
+    const int parts = d / (2 * rope::Vec<T>::kN);
+    const long long threads = static_cast<long long>(tokens) * parts, blocks = (threads + rope::kThreads - 1) / rope::kThreads;
+    if (blocks > INT_MAX) return ATTNW_ERR_BAD_SHAPE;
+    const int each = heads_each(threads, H, dev->sm_count);
+    const rope::Rows rows{X, Y, x_strides[0], x_strides[2], x_strides[1], y_strides[0], y_strides[2], y_strides[1], H};
+    const rope::Turn turn{positions, frequencies, rotary, amplitude, inverse ? -1.0f : 1.0f};
+    const auto kernel = layout == 0 ? rope::rope_kernel<T, true> : rope::rope_kernel<T, false>;
+    if (launch_overlapped_3d(kernel, static_cast<unsigned>(blocks), static_cast<unsigned>((H + each - 1) / each), 1, rope::kThreads,
+                             static_cast<cudaStream_t>(stream), rows, turn, static_cast<long long>(tokens), N, parts, each) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return ATTNW_OK;
+}
+
+// Host-only checks of the cache's description.
+int check_cache(const attnw_cache* c) {
+    if (!c || !c->K || !c->V || !c->table || !c->lengths) return ATTNW_ERR_NULL_POINTER;
+    if (c->pages < 1 || c->kv_heads < 1 || c->page < 1 || c->d < 1 || c->sequences < 1 || c->table_width < 1) return ATTNW_ERR_BAD_SHAPE;
+    if (c->d != 64 && c->d != 128) return ATTNW_ERR_UNSUPPORTED;
+    if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) != 0) return ATTNW_ERR_UNSUPPORTED;
+    if (static_cast<long long>(c->pages) * c->kv_heads >= INT_MAX) return ATTNW_ERR_BAD_SHAPE;
+    if (static_cast<long long>(c->sequences) * c->kv_heads > 65535) return ATTNW_ERR_BAD_SHAPE;
+    if (static_cast<long long>(c->table_width) * c->page > (1 << 28)) return ATTNW_ERR_BAD_SHAPE;
+    if (!aligned16(c->K) || !aligned16(c->V) || !aligned4(c->table) || !aligned4(c->lengths)) return ATTNW_ERR_MISALIGNED;
+    return ATTNW_OK;
+}
+
+struct Span {
+    const void* p;
+    unsigned long long bytes;
+};
+unsigned long long cache_bytes(const attnw_cache* c) {
+    return 2ull * static_cast<unsigned long long>(c->pages) * c->kv_heads * c->page * c->d;
+}
+bool crosses(const Span& a, const Span& b) { return a.p && b.p && overlaps(a.p, a.bytes, b.p, b.bytes); }
+Span span_of(const Extent& e) { return {reinterpret_cast<const void*>(e.begin), static_cast<unsigned long long>(e.end - e.begin)}; }
+
+paged::Cache view_of(const attnw_cache* c) {
+    int shift = 0;
+    while ((1 << shift) < c->page) ++shift;
+    return {static_cast<__nv_bfloat16*>(c->K), static_cast<__nv_bfloat16*>(c->V), c->table, c->lengths, c->pages, c->kv_heads, shift, c->d, c->sequences,
+            c->table_width};
+}
+
+int append_entry(const attnw_cache* c, const void* Q, const void* K, const void* V, void* Q_out, const long long* strides, const int* starts,
+                 const int* positions, const double* frequencies, int tokens, int heads, int rotary, int layout, float amplitude, void* stream) {
+    int rc = check_cache(c);
+    if (rc != ATTNW_OK) return rc;
+    if (!K || !V || !strides || !starts || (!Q) != (!Q_out) || (rotary > 0 && (!positions || !frequencies))) return ATTNW_ERR_NULL_POINTER;
+    if (tokens < 1 || (Q && heads < 1) || heads > 65535) return ATTNW_ERR_BAD_SHAPE;
+    rc = check_turn(frequencies, rotary, c->d, layout, amplitude);
+    if (rc != ATTNW_OK) return rc;
+    const long long q_sizes[2] = {tokens, Q ? heads : 1}, kv_sizes[2] = {tokens, c->kv_heads};
+    rc = check_strides(strides + 2, kv_sizes, 2, 2, false);
+    if (rc == ATTNW_OK) rc = check_strides(strides + 4, kv_sizes, 2, 2, false);
+    if (rc == ATTNW_OK && Q) rc = check_strides(strides, q_sizes, 2, 2, false);
+    if (rc == ATTNW_OK && Q) rc = check_strides(strides + 6, q_sizes, 2, 2, true);
+    if (rc != ATTNW_OK) return rc;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(Q) || !aligned16(Q_out) || !aligned4(starts) || !aligned4(positions)) return ATTNW_ERR_MISALIGNED;
+    const Extent k = extent_of(K, strides + 2, kv_sizes, 2, 0, c->d, 2), v = extent_of(V, strides + 4, kv_sizes, 2, 0, c->d, 2);
+    const Span caches[2] = {{c->K, cache_bytes(c)}, {c->V, cache_bytes(c)}};
+    const Span index[5] = {{c->table, 4ull * c->sequences * c->table_width}, {c->lengths, 4ull * c->sequences}, {starts, 4ull * (c->sequences + 1ull)},
+                           {positions, 4ull * tokens}, {frequencies, 4ull * rotary}};
+    if (crosses(caches[0], caches[1])) return ATTNW_ERR_ALIASING;
+    for (const Span& s : caches) {
+        if (crosses(s, span_of(k)) || crosses(s, span_of(v))) return ATTNW_ERR_ALIASING;
+        for (const Span& i : index)
+            if (crosses(s, i)) return ATTNW_ERR_ALIASING;
+    }
+    if (Q) {
+        const Extent q = extent_of(Q, strides, q_sizes, 2, 0, c->d, 2), o = extent_of(Q_out, strides + 6, q_sizes, 2, 0, c->d, 2);
+        bool in_place = Q == Q_out;
+        for (int i = 0; i < 2; ++i) in_place = in_place && (q_sizes[i] == 1 || strides[i] == strides[6 + i]);
+        if ((!in_place && may_overlap(q, o)) || may_overlap(k, o) || may_overlap(v, o)) return ATTNW_ERR_ALIASING;
+        for (const Span& s : caches)
+            if (crosses(s, span_of(q)) || crosses(s, span_of(o))) return ATTNW_ERR_ALIASING;
+        for (const Span& i : index)
+            if (crosses(span_of(o), i)) return ATTNW_ERR_ALIASING;
+    }
+    DeviceInfo* dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != ATTNW_OK) return rc;
+    const int parts = c->d / 16;
+    const long long threads = static_cast<long long>(tokens) * parts, blocks = (threads + rope::kThreads - 1) / rope::kThreads;
+    const int rows = (Q ? heads : 0) + 2 * c->kv_heads, each = std::min(heads_each(threads, rows, dev->sm_count), std::max(Q ? heads : 1, c->kv_heads));
+    const int q_groups = Q ? (heads + each - 1) / each : 0, kv_groups = (c->kv_heads + each - 1) / each;
+    if (q_groups + 2 * kv_groups > 65535) return ATTNW_ERR_BAD_SHAPE;
+    const rope::Rows q{Q, Q_out, 0, strides[0], strides[1], 0, strides[6], strides[7], heads}, k_rows{K, nullptr, 0, strides[2], strides[3], 0, 0, 0, c->kv_heads},
+        v_rows{V, nullptr, 0, strides[4], strides[5], 0, 0, 0, c->kv_heads};
+    const rope::Turn turn{rotary > 0 ? positions : nullptr, frequencies, rotary, amplitude, 1.0f};
+    const auto kernel = layout == 0 ? rope::append_kernel<true> : rope::append_kernel<false>;
+    if (launch_overlapped_3d(kernel, static_cast<unsigned>(blocks), static_cast<unsigned>(q_groups + 2 * kv_groups), 1, rope::kThreads,
+                             static_cast<cudaStream_t>(stream), q, k_rows, v_rows, view_of(c), starts, turn, tokens, parts, each, q_groups,
+                             kv_groups) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return ATTNW_OK;
+}
+
+// Where the parts of attn_paged's workspace begin.
+struct PagedWorkspace {
+    unsigned long long lse = 0, bytes = 0;
+};
+PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool weigh, bool lse_given) {
+    PagedWorkspace w;
+    if (weigh && !lse_given) w.bytes = 4ull * tokens * heads;
+    (void)c;
+    return w;
+}
+
+int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
+                void* workspace, unsigned long long workspace_bytes, int tokens, int heads, float scale, void* stream) {
+    int rc = check_cache(c);
+    if (rc != ATTNW_OK) return rc;
+    if (!Q || !q_strides || !starts || !O || (!mass) != (!mass_out)) return ATTNW_ERR_NULL_POINTER;
+    if (tokens < 1 || heads < 1 || heads % c->kv_heads != 0) return ATTNW_ERR_BAD_SHAPE;
+    if (!(scale >= 0.0f) || !std::isfinite(scale)) return ATTNW_ERR_BAD_SHAPE;
+    if (heads / c->kv_heads > 128) return ATTNW_ERR_UNSUPPORTED;
+    if (static_cast<long long>(tokens) * heads > INT_MAX / 4) return ATTNW_ERR_BAD_SHAPE;
+    const long long sizes[2] = {tokens, heads};
+    rc = check_strides(q_strides, sizes, 2, 2, true);  // (a tensor map has no broadcast dimensions)
+    if (rc != ATTNW_OK) return rc;
+    if (!aligned16(Q) || !aligned16(O) || !aligned4(starts) || !aligned4(lse) || !aligned4(mass) || !aligned4(mass_out)) return ATTNW_ERR_MISALIGNED;
+    const unsigned long long capacity = static_cast<unsigned long long>(c->table_width) * c->page, weights = 4ull * c->sequences * c->kv_heads * capacity;
+    const PagedWorkspace w = paged_workspace(c, tokens, heads, mass != nullptr, lse != nullptr);
+    if (w.bytes > 0 && !workspace) return ATTNW_ERR_NULL_POINTER;
+    if (workspace_bytes < w.bytes) return ATTNW_ERR_BAD_SHAPE;
+    if (w.bytes > 0 && !aligned16(workspace)) return ATTNW_ERR_MISALIGNED;
+    const Span out[4] = {{O, 2ull * tokens * heads * c->d}, {lse, 4ull * tokens * heads}, {mass_out, weights}, {w.bytes ? workspace : nullptr, w.bytes}};
+    const Span in[6] = {{c->K, cache_bytes(c)}, {c->V, cache_bytes(c)}, {c->table, 4ull * c->sequences * c->table_width}, {c->lengths, 4ull * c->sequences},
+                        {starts, 4ull * (c->sequences + 1ull)}, span_of(extent_of(Q, q_strides, sizes, 2, 0, c->d, 2))};
+    for (int i = 0; i < 4; ++i) {
+        for (const Span& s : in)
+            if (crosses(out[i], s)) return ATTNW_ERR_ALIASING;
+        for (int j = 0; j < i; ++j)
+            if (crosses(out[i], out[j])) return ATTNW_ERR_ALIASING;
+        if (crosses(out[i], {mass, weights}) && !(out[i].p == mass_out && mass == mass_out)) return ATTNW_ERR_ALIASING;
+    }
+    DeviceInfo* dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != ATTNW_OK) return rc;
+    const paged::Cache view = view_of(c);
+    float* own_lse = lse ? lse : mass ? reinterpret_cast<float*>(static_cast<char*>(workspace) + w.lse) : nullptr;
+    const auto* q = static_cast<const __nv_bfloat16*>(Q);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const long long warps = static_cast<long long>(tokens) * heads;
+    cudaError_t e = launch_overlapped_3d(c->d == 64 ? pa0::attn_kernel<64> : pa0::attn_kernel<128>, static_cast<unsigned>((warps + pa0::kWarps - 1) / pa0::kWarps),
+                                         1, 1, pa0::kWarps * 32, s, q, q_strides[0], q_strides[1], view, starts, static_cast<__nv_bfloat16*>(O), own_lse,
+                                         tokens, heads, scale);
+    if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (e == cudaSuccess && mass) {
+        e = launch_overlapped_3d(c->d == 64 ? pa0::mass_kernel<64> : pa0::mass_kernel<128>, static_cast<unsigned>((capacity + 127) / 128),
+                                 static_cast<unsigned>(c->sequences * c->kv_heads), 1, 128, s, q, q_strides[0], q_strides[1], view, starts, own_lse, mass,
+                                 mass_out, tokens, heads, scale, static_cast<int>(capacity));
+        if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    return ATTNW_OK;
+}
+
+int evict_entry(const attnw_cache* c, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out, int budget,
+                int recent, void* stream) {
+    int rc = check_cache(c);
+    if (rc != ATTNW_OK) return rc;
+    if (!mass || !mass_out || !kept || !lengths_out) return ATTNW_ERR_NULL_POINTER;
+    const bool in_place = !table_out || table_out == c->table;
+    const int width_out = table_out ? table_out_width : c->table_width;
+    if (width_out < 1 || (table_out == c->table && width_out != c->table_width)) return ATTNW_ERR_BAD_SHAPE;
+    const long long capacity = static_cast<long long>(c->table_width) * c->page, capacity_out = static_cast<long long>(width_out) * c->page;
+    if (budget < 1 || recent < 0 || recent > budget || budget > capacity_out || capacity_out > (1 << 28)) return ATTNW_ERR_BAD_SHAPE;
+    if (!aligned4(mass) || !aligned4(mass_out) || !aligned4(kept) || !aligned4(lengths_out) || !aligned4(table_out)) return ATTNW_ERR_MISALIGNED;
+    const unsigned long long rows = static_cast<unsigned long long>(c->sequences) * c->kv_heads;
+    const Span out[5] = {{c->K, cache_bytes(c)}, {c->V, cache_bytes(c)}, {mass_out, 4ull * rows * capacity_out}, {kept, 4ull * rows * budget},
+                         {lengths_out, 4ull * c->sequences}};
+    const Span in[4] = {{c->table, 4ull * c->sequences * c->table_width}, {c->lengths, 4ull * c->sequences},
+                        {table_out, table_out ? 4ull * c->sequences * width_out : 0}, {mass, 4ull * rows * capacity}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (crosses(out[i], out[j])) return ATTNW_ERR_ALIASING;
+        for (const Span& s : in)
+            if (crosses(out[i], s) && !(i == 2 && s.p == mass && mass == mass_out && capacity == capacity_out)) return ATTNW_ERR_ALIASING;
+    }
+    DeviceInfo* dev = nullptr;
+    rc = current_device(&dev);
+    if (rc != ATTNW_OK) return rc;
+    const paged::Cache view = view_of(c);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_overlapped_3d(evict::evict_select_kernel, static_cast<unsigned>(rows), 1, 1, evict::kSelectThreads, s, view, mass, mass_out, kept,
+                                         lengths_out, budget, recent, static_cast<int>(capacity), static_cast<int>(capacity_out));
+    if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (e == cudaSuccess) {
+        // In place: as many CTAs a row as fill the device twice, of at least 32 bytes of each key.
+        int slices = 1;
+        while (in_place && slices < c->d / 16 && static_cast<long long>(rows) * 2 * slices < 2 * dev->sm_count) slices *= 2;
+        const int keys = evict::kMoveThreads * evict::kFlight / (c->d / 8 / slices), steps = in_place ? 1 : (budget + keys - 1) / keys;
+        const auto kernel = in_place ? evict::evict_move_kernel<true> : evict::evict_move_kernel<false>;
+        e = launch_overlapped_3d(kernel, static_cast<unsigned>(steps * slices), static_cast<unsigned>(rows), 2, evict::kMoveThreads, s, view,
+                                 in_place ? c->table : table_out, width_out, kept, budget, slices);
+        if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    return ATTNW_OK;
+}
+
+}  // namespace

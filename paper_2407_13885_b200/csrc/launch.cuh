@@ -62,4 +62,19 @@ inline cudaError_t launch_overlapped(void (*kernel)(Params...), unsigned grid, u
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
+// The same with a grid of three dimensions, no cluster and no dynamic shared memory.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_overlapped_3d(void (*kernel)(Params...), unsigned x, unsigned y, unsigned z, unsigned block, cudaStream_t stream, Args... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(x, y, z);
+    cfg.blockDim = dim3(block, 1, 1);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 }  // namespace attnw

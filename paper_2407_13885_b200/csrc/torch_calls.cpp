@@ -12,7 +12,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <cstdint>
+#include <cstring>
+#include <initializer_list>
+#include <string>
 
 #include "../../include/attnw.h"
 
@@ -249,6 +253,344 @@ PyObject* py_softmax_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the paged cache ----------------------------------------------------------------------------------------------------------
+
+bool value_error(const char* text) {
+    PyErr_SetString(PyExc_ValueError, text);
+    return false;
+}
+
+// As tensor_arg, but for strided tensors of `dim` dimensions whose last one is contiguous.
+const at::Tensor* strided_arg(PyObject* obj, const char* name, at::ScalarType type, const char* type_name, int dim, const at::Tensor* like) {
+    if (!THPVariable_Check(obj) || !THPVariable_Unpack(obj).is_cuda()) {
+        PyErr_Format(PyExc_TypeError, "%s must be a CUDA tensor", name);
+        return nullptr;
+    }
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (t.scalar_type() != type) {
+        PyErr_Format(PyExc_TypeError, "%s must have dtype %s, got %s", name, type_name, at::toString(t.scalar_type()));
+        return nullptr;
+    }
+    if (t.dim() != dim || (t.size(dim - 1) > 1 && t.stride(dim - 1) != 1)) {
+        PyErr_Format(PyExc_ValueError, "%s must have %d dimensions, the last one contiguous", name, dim);
+        return nullptr;
+    }
+    if (like && t.device() != like->device()) {
+        PyErr_Format(PyExc_ValueError, "%s must be on %s like the other tensors, got %s", name, like->device().str().c_str(),
+                     t.device().str().c_str());
+        return nullptr;
+    }
+    return &t;
+}
+
+// A contiguous index or weight tensor of the given sizes (-1: any, written back).
+const at::Tensor* plain_arg(PyObject* obj, const char* name, at::ScalarType type, const char* type_name, std::initializer_list<int64_t> sizes,
+                            const at::Tensor* like) {
+    const at::Tensor* t = tensor_arg(obj, name, type, type_name, like);
+    if (!t) return nullptr;
+    bool fits = t->dim() == static_cast<int64_t>(sizes.size());
+    int i = 0;
+    for (const int64_t n : sizes) {
+        if (!fits) break;
+        fits = n < 0 || t->size(i) == n;
+        ++i;
+    }
+    if (!fits) {
+        std::string want;
+        for (const int64_t n : sizes) want += (want.empty() ? "" : ", ") + (n < 0 ? std::string("any") : std::to_string(n));
+        PyErr_Format(PyExc_ValueError, "%s must be [%s]", name, want.c_str());
+        return nullptr;
+    }
+    return t;
+}
+const at::Tensor* int_arg(PyObject* obj, const char* name, std::initializer_list<int64_t> sizes, const at::Tensor* like) {
+    return plain_arg(obj, name, at::kInt, "torch.int32", sizes, like);
+}
+const at::Tensor* f32_arg(PyObject* obj, const char* name, std::initializer_list<int64_t> sizes, const at::Tensor* like) {
+    return plain_arg(obj, name, at::kFloat, "torch.float32", sizes, like);
+}
+
+bool small(std::initializer_list<int64_t> sizes) {
+    for (const int64_t n : sizes)
+        if (n > INT_MAX) return value_error("a size is above 2^31 - 1");
+    return true;
+}
+
+bool int_value(PyObject* obj, int* out) {
+    const long v = PyLong_AsLong(obj);
+    if (v == -1 && PyErr_Occurred()) return false;
+    if (v < INT_MIN || v > INT_MAX) return value_error("a size is above 2^31 - 1");
+    *out = static_cast<int>(v);
+    return true;
+}
+
+bool layout_arg(PyObject* obj, int* out) {
+    const char* s = PyUnicode_Check(obj) ? PyUnicode_AsUTF8(obj) : nullptr;
+    if (s && !strcmp(s, "half")) {
+        *out = 0;
+        return true;
+    }
+    if (s && !strcmp(s, "interleaved")) {
+        *out = 1;
+        return true;
+    }
+    if (PyErr_Occurred()) return false;
+    return value_error("layout must be \"half\" or \"interleaved\"");
+}
+
+// K_cache, V_cache, table and lengths at a[0 ... 3].
+bool cache_arg(PyObject* const* a, attnw_cache* c, const at::Tensor** k_cache) {
+    const at::Tensor *k, *v, *table, *lengths;
+    if (!(k = bf16_arg(a[0], "K_cache", nullptr)) || !(v = bf16_arg(a[1], "V_cache", k))) return false;
+    if (k->dim() != 4 || k->sizes() != v->sizes()) return value_error("K_cache and V_cache must both be [pages, kv_heads, page, d]");
+    if (!(table = int_arg(a[2], "table", {-1, -1}, k)) || !(lengths = int_arg(a[3], "lengths", {table->size(0)}, k))) return false;
+    if (!small({k->size(0), k->size(1), k->size(2), k->size(3), table->size(0), table->size(1)})) return false;
+    c->K = k->data_ptr();
+    c->V = v->data_ptr();
+    c->table = static_cast<const int*>(table->data_ptr());
+    c->lengths = static_cast<const int*>(lengths->data_ptr());
+    c->pages = static_cast<int>(k->size(0));
+    c->kv_heads = static_cast<int>(k->size(1));
+    c->page = static_cast<int>(k->size(2));
+    c->d = static_cast<int>(k->size(3));
+    c->sequences = static_cast<int>(table->size(0));
+    c->table_width = static_cast<int>(table->size(1));
+    *k_cache = k;
+    return true;
+}
+
+// Scratch memory of one call on `stream`: it belongs to that stream, so that whoever gets it next runs behind the call.
+at::Tensor scratch(int64_t bytes, void* stream, const at::Tensor& like) {
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
+    return at::empty({bytes}, like.options().dtype(at::kByte).requires_grad(false));
+}
+
+PyObject* given_or_new(PyObject* given, at::Tensor&& made) { return given != Py_None ? Py_NewRef(given) : THPVariable_Wrap(std::move(made)); }
+
+// rope(X, positions, frequencies, layout, amplitude, inverse, out, stream)
+PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!count_is(n, 8)) return nullptr;
+    const bool f32 = THPVariable_Check(a[0]) && THPVariable_Unpack(a[0]).scalar_type() == at::kFloat;
+    const at::ScalarType type = f32 ? at::kFloat : at::kBFloat16;
+    const char* type_name = f32 ? "torch.float32" : "torch.bfloat16";
+    const at::Tensor *x, *positions, *frequencies;
+    if (!(x = strided_arg(a[0], "X", type, type_name, 4, nullptr))) return nullptr;
+    const int64_t B = x->size(0), H = x->size(1), N = x->size(2), d = x->size(3);
+    if (!small({B, H, N, d})) return nullptr;
+    if (!(positions = int_arg(a[1], "positions", {B, N}, x)) ||
+        !(frequencies = plain_arg(a[2], "frequencies", at::kDouble, "torch.float64", {-1}, x)))
+        return nullptr;
+    if (!small({2 * frequencies->size(0)})) return nullptr;
+    int layout;
+    float amplitude;
+    if (!layout_arg(a[3], &layout) || !float_arg(a[4], &amplitude)) return nullptr;
+    const int inverse = PyObject_IsTrue(a[5]);
+    if (inverse < 0) return nullptr;
+    const void* x_ptr = x->data_ptr();
+    const auto* p_ptr = static_cast<const int*>(positions->data_ptr());
+    const auto* f_ptr = static_cast<const double*>(frequencies->data_ptr());
+    at::Tensor y;
+    if (a[6] == Py_None) {
+        y = at::empty(x->sizes(), x->options().requires_grad(false));
+    } else {
+        const at::Tensor* t = strided_arg(a[6], "out", type, type_name, 4, x);
+        if (!t) return nullptr;
+        if (t->sizes() != x->sizes()) {
+            value_error("out must be [B, H, N, d] like X");
+            return nullptr;
+        }
+        y = *t;
+    }
+    const c10::cuda::CUDAGuard guard(x->device());
+    void* stream;
+    if (!stream_arg(a[7], &stream)) return nullptr;
+    const long long xs[3] = {x->stride(0), x->stride(1), x->stride(2)}, ys[3] = {y.stride(0), y.stride(1), y.stride(2)};
+    const auto entry = f32 ? attnw_rope_f32 : attnw_rope;
+    void* y_ptr = y.data_ptr();
+    const int rotary = static_cast<int>(2 * frequencies->size(0));
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = entry(x_ptr, p_ptr, f_ptr, y_ptr, static_cast<int>(B), static_cast<int>(H), static_cast<int>(N), static_cast<int>(d), rotary, xs, ys, layout,
+               inverse, amplitude, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != ATTNW_OK) return failed(rc, "attnw_rope");
+    return given_or_new(a[6], std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_append(K_cache, V_cache, table, lengths, starts, Q, K, V, positions, frequencies, layout, amplitude, Q_out, stream)
+PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!count_is(n, 14)) return nullptr;
+    attnw_cache c;
+    const at::Tensor *cache, *starts, *q = nullptr, *k, *v, *positions = nullptr, *frequencies = nullptr;
+    if (!cache_arg(a, &c, &cache) || !(starts = int_arg(a[4], "starts", {c.sequences + int64_t{1}}, cache))) return nullptr;
+    if (!(k = strided_arg(a[6], "K", at::kBFloat16, "torch.bfloat16", 3, cache)) || !(v = strided_arg(a[7], "V", at::kBFloat16, "torch.bfloat16", 3, cache)))
+        return nullptr;
+    if (k->sizes() != v->sizes() || k->size(1) != c.kv_heads || k->size(2) != c.d) {
+        value_error("K and V must both be [tokens, kv_heads, d]");
+        return nullptr;
+    }
+    const int64_t tokens = k->size(0);
+    if (a[5] != Py_None) {
+        if (!(q = strided_arg(a[5], "Q", at::kBFloat16, "torch.bfloat16", 3, cache))) return nullptr;
+        if (q->size(0) != tokens || q->size(2) != c.d) {
+            value_error("Q must be [tokens, heads, d]");
+            return nullptr;
+        }
+    } else if (a[12] != Py_None) {
+        value_error("Q_out needs Q");
+        return nullptr;
+    }
+    if ((a[8] == Py_None) != (a[9] == Py_None)) {
+        value_error("positions and frequencies come together");
+        return nullptr;
+    }
+    if (a[8] != Py_None && (!(positions = int_arg(a[8], "positions", {tokens}, cache)) ||
+                            !(frequencies = plain_arg(a[9], "frequencies", at::kDouble, "torch.float64", {-1}, cache))))
+        return nullptr;
+    const int64_t rotary = frequencies ? 2 * frequencies->size(0) : 0;
+    if (!small({tokens, q ? q->size(1) : 0, rotary})) return nullptr;
+    int layout;
+    float amplitude;
+    if (!layout_arg(a[10], &layout) || !float_arg(a[11], &amplitude)) return nullptr;
+    const void *q_ptr = q ? q->data_ptr() : nullptr, *k_ptr = k->data_ptr(), *v_ptr = v->data_ptr();
+    const auto* s_ptr = static_cast<const int*>(starts->data_ptr());
+    const auto* p_ptr = positions ? static_cast<const int*>(positions->data_ptr()) : nullptr;
+    const auto* f_ptr = frequencies ? static_cast<const double*>(frequencies->data_ptr()) : nullptr;
+    at::Tensor out;
+    if (q && a[12] == Py_None) {
+        out = at::empty(q->sizes(), q->options().requires_grad(false));
+    } else if (q) {
+        const at::Tensor* t = strided_arg(a[12], "Q_out", at::kBFloat16, "torch.bfloat16", 3, cache);
+        if (!t) return nullptr;
+        if (t->sizes() != q->sizes()) {
+            value_error("Q_out must be [tokens, heads, d] like Q");
+            return nullptr;
+        }
+        out = *t;
+    }
+    const c10::cuda::CUDAGuard guard(cache->device());
+    void* stream;
+    if (!stream_arg(a[13], &stream)) return nullptr;
+    const long long strides[8] = {q ? q->stride(0) : 0, q ? q->stride(1) : 0, k->stride(0), k->stride(1), v->stride(0), v->stride(1),
+                                  q ? out.stride(0) : 0, q ? out.stride(1) : 0};
+    void* o_ptr = q ? out.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = attnw_cache_append(&c, q_ptr, k_ptr, v_ptr, o_ptr, strides, s_ptr, p_ptr, f_ptr, static_cast<int>(tokens),
+                            q ? static_cast<int>(q->size(1)) : 0, static_cast<int>(rotary), layout, amplitude, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != ATTNW_OK) return failed(rc, "attnw_cache_append");
+    if (!q) Py_RETURN_NONE;
+    return given_or_new(a[12], std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_paged(K_cache, V_cache, table, lengths, starts, Q, scale, O, lse, mass, mass_out, stream)
+PyObject* py_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!count_is(n, 12)) return nullptr;
+    attnw_cache c;
+    const at::Tensor *cache, *starts, *q, *lse = nullptr, *mass = nullptr;
+    if (!cache_arg(a, &c, &cache) || !(starts = int_arg(a[4], "starts", {c.sequences + int64_t{1}}, cache))) return nullptr;
+    if (!(q = strided_arg(a[5], "Q", at::kBFloat16, "torch.bfloat16", 3, cache))) return nullptr;
+    if (q->size(2) != c.d) {
+        value_error("Q must be [tokens, heads, d]");
+        return nullptr;
+    }
+    const int64_t tokens = q->size(0), heads = q->size(1), capacity = int64_t{c.table_width} * c.page;
+    if (!small({tokens, heads})) return nullptr;
+    float scale;
+    if (!float_arg(a[6], &scale)) return nullptr;
+    if (a[8] != Py_None && !(lse = f32_arg(a[8], "lse", {tokens, heads}, cache))) return nullptr;
+    if (a[9] != Py_None && !(mass = f32_arg(a[9], "mass", {c.sequences, c.kv_heads, capacity}, cache))) return nullptr;
+    if (!mass && a[10] != Py_None) {
+        value_error("mass_out needs mass");
+        return nullptr;
+    }
+    const void* q_ptr = q->data_ptr();
+    const auto* s_ptr = static_cast<const int*>(starts->data_ptr());
+    float* lse_ptr = lse ? static_cast<float*>(lse->data_ptr()) : nullptr;
+    const float* mass_ptr = mass ? static_cast<const float*>(mass->data_ptr()) : nullptr;
+    at::Tensor o, mass_out;
+    if (!output_arg(a[7], "O", q->sizes(), at::kBFloat16, false, true, "[tokens, heads, d]", *q, &o)) return nullptr;
+    if (mass && a[10] == Py_None) {
+        mass_out = at::empty(mass->sizes(), mass->options().requires_grad(false));
+    } else if (mass) {
+        const at::Tensor* t = f32_arg(a[10], "mass_out", {c.sequences, c.kv_heads, capacity}, cache);
+        if (!t) return nullptr;
+        mass_out = *t;
+    }
+    const c10::cuda::CUDAGuard guard(cache->device());
+    void* stream;
+    if (!stream_arg(a[11], &stream)) return nullptr;
+    const long long strides[2] = {q->stride(0), q->stride(1)};
+    const long long bytes = attn_paged_workspace(&c, static_cast<int>(tokens), static_cast<int>(heads), mass ? 1 : 0);
+    at::Tensor workspace;
+    if (bytes > 0) workspace = scratch(bytes, stream, *cache);
+    void *o_ptr = o.data_ptr(), *w_ptr = bytes > 0 ? workspace.data_ptr() : nullptr;
+    float* out_ptr = mass ? static_cast<float*>(mass_out.data_ptr()) : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = attn_paged(&c, q_ptr, strides, s_ptr, o_ptr, lse_ptr, mass_ptr, out_ptr, w_ptr, bytes, static_cast<int>(tokens), static_cast<int>(heads), scale,
+                    stream);
+    Py_END_ALLOW_THREADS
+    if (rc != ATTNW_OK) return failed(rc, "attn_paged");
+    PyObject* po = given_or_new(a[7], std::move(o));
+    if (!mass || !po) return po;
+    PyObject* pm = given_or_new(a[10], std::move(mass_out));
+    PyObject* pair = pm ? PyTuple_Pack(2, po, pm) : nullptr;
+    Py_DECREF(po);
+    Py_XDECREF(pm);
+    return pair;
+    END_HANDLE_TH_ERRORS
+}
+
+// cache_evict(K_cache, V_cache, table, lengths, mass, budget, recent, table_out, mass_out, stream)
+PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!count_is(n, 10)) return nullptr;
+    attnw_cache c;
+    const at::Tensor *cache, *mass, *table_out = nullptr;
+    if (!cache_arg(a, &c, &cache) || !(mass = f32_arg(a[4], "mass", {c.sequences, c.kv_heads, int64_t{c.table_width} * c.page}, cache))) return nullptr;
+    int budget, recent;
+    if (!int_value(a[5], &budget) || !int_value(a[6], &recent)) return nullptr;
+    if (a[7] != Py_None && !(table_out = int_arg(a[7], "table_out", {c.sequences, -1}, cache))) return nullptr;
+    const int64_t width = table_out ? table_out->size(1) : c.table_width, capacity = width * c.page;
+    if (!small({width, capacity})) return nullptr;
+    const float* mass_ptr = static_cast<const float*>(mass->data_ptr());
+    const int* out_table = table_out ? static_cast<const int*>(table_out->data_ptr()) : nullptr;
+    const auto ints = cache->options().dtype(at::kInt).requires_grad(false);
+    at::Tensor mass_out;
+    if (a[8] == Py_None) {
+        mass_out = at::empty({c.sequences, c.kv_heads, capacity}, mass->options().requires_grad(false));
+    } else {
+        const at::Tensor* t = f32_arg(a[8], "mass_out", {c.sequences, c.kv_heads, capacity}, cache);
+        if (!t) return nullptr;
+        mass_out = *t;
+    }
+    at::Tensor kept = at::empty({c.sequences, c.kv_heads, budget > 0 ? budget : 0}, ints), lengths_out = at::empty({c.sequences}, ints);
+    const c10::cuda::CUDAGuard guard(cache->device());
+    void* stream;
+    if (!stream_arg(a[9], &stream)) return nullptr;
+    float* out_ptr = static_cast<float*>(mass_out.data_ptr());
+    int *kept_ptr = static_cast<int*>(kept.data_ptr()), *length_ptr = static_cast<int*>(lengths_out.data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = attnw_cache_evict(&c, out_table, static_cast<int>(width), mass_ptr, out_ptr, kept_ptr, length_ptr, budget, recent, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != ATTNW_OK) return failed(rc, "attnw_cache_evict");
+    PyObject *pk = THPVariable_Wrap(std::move(kept)), *pl = THPVariable_Wrap(std::move(lengths_out)), *pm = given_or_new(a[8], std::move(mass_out));
+    PyObject* all = pk && pl && pm ? PyTuple_Pack(3, pk, pl, pm) : nullptr;
+    Py_XDECREF(pk);
+    Py_XDECREF(pl);
+    Py_XDECREF(pm);
+    return all;
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* py_set_error(PyObject*, PyObject* type) {
     Py_XSETREF(g_error, Py_NewRef(type));
     Py_RETURN_NONE;
@@ -264,6 +606,13 @@ PyMethodDef g_methods[] = {
     {"attn_fused", fast(py_attn_fused), METH_FASTCALL, "attn_fused(Q, K, V, scale, O, stream)"},
     {"project_qk", fast(py_project_qk), METH_FASTCALL, "project_qk(X, Wq, Wk, Q, K, stream)"},
     {"softmax_rows", fast(py_softmax_rows), METH_FASTCALL, "softmax_rows(S, P, out_dtype, stream)"},
+    {"rope", fast(py_rope), METH_FASTCALL, "rope(X, positions, frequencies, layout, amplitude, inverse, out, stream)"},
+    {"cache_append", fast(py_cache_append), METH_FASTCALL,
+     "cache_append(K_cache, V_cache, table, lengths, starts, Q, K, V, positions, frequencies, layout, amplitude, Q_out, stream)"},
+    {"attn_paged", fast(py_attn_paged), METH_FASTCALL,
+     "attn_paged(K_cache, V_cache, table, lengths, starts, Q, scale, O, lse, mass, mass_out, stream)"},
+    {"cache_evict", fast(py_cache_evict), METH_FASTCALL,
+     "cache_evict(K_cache, V_cache, table, lengths, mass, budget, recent, table_out, mass_out, stream)"},
     {"set_error", py_set_error, METH_O, "the exception type for attnw status codes"},
     {nullptr, nullptr, 0, nullptr},
 };
