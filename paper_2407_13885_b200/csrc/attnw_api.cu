@@ -25,7 +25,8 @@
 #include "softmax_rows_smem.cuh"
 #include "rope.cuh"
 #include "cache_evict.cuh"
-#include "attn_paged_simple.cuh"
+#include "attn_paged.cuh"
+#include "paged_mass.cuh"
 
 namespace {
 
@@ -169,6 +170,19 @@ int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, size_t esize, const v
     CUresult r = g_encode_tiled.load(std::memory_order_relaxed)(map, dtype, 3, const_cast<void*>(base), dims, strides, box, elem_strides,
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ATTNW_OK : ATTNW_ERR_CUDA;
+}
+
+// bfloat16 [dim3][dim2][dim1][dim0] with the strides given in bytes, box {box0, box1, box2, box3}, 128-byte swizzle (box0 == 64).
+int encode_4d(CUtensorMap* map, const void* base, uint64_t dim0, uint64_t dim1, uint64_t dim2, uint64_t dim3, uint64_t stride1, uint64_t stride2,
+              uint64_t stride3, uint32_t box0, uint32_t box1, uint32_t box2, uint32_t box3) {
+    const cuuint64_t dims[4] = {dim0, dim1, dim2, dim3};
+    const cuuint64_t strides[3] = {stride1, stride2, stride3};
+    const cuuint32_t box[4] = {box0, box1, box2, box3};
+    const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+    CUresult r = g_encode_tiled.load(std::memory_order_relaxed)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, elem_strides,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? ATTNW_OK : ATTNW_ERR_CUDA;
 }
 
@@ -1187,8 +1201,8 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
 }
 
 long long attn_paged_workspace(const attnw_cache* cache, int tokens, int heads, int weigh) {
-    if (!cache || tokens < 1 || heads < 1) return 0;
-    return static_cast<long long>(paged_workspace(cache, tokens, heads, weigh != 0, false).bytes);
+    if (!cache || tokens < 1 || heads < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 || heads / cache->kv_heads > 128) return 0;
+    return static_cast<long long>(paged_workspace(cache, tokens, heads, weigh != 0).bytes);
 }
 
 int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,

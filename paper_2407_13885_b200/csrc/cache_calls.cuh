@@ -197,13 +197,70 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
 
 // Where the parts of attn_paged's workspace begin.
 struct PagedWorkspace {
-    unsigned long long lse = 0, bytes = 0;
+    unsigned long long lse = 0, plan = 0, stats = 0, o = 0, bytes = 0;
+    long long rows = 0;  // of the segments' parts; 0: no block is long enough to be cut
 };
-PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool weigh, bool lse_given) {
+PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool weigh) {
     PagedWorkspace w;
-    if (weigh && !lse_given) w.bytes = 4ull * tokens * heads;
-    (void)c;
+    auto take = [&w](unsigned long long bytes) {
+        const unsigned long long at = w.bytes;
+        w.bytes = (w.bytes + bytes + 255) / 256 * 256;
+        return at;
+    };
+    if (weigh) w.lse = take(4ull * tokens * heads);
+    const int group = heads / c->kv_heads, tile_tokens = 128 / group;
+    const long long tiles = (static_cast<long long>(c->table_width) * c->page + kTile - 1) / kTile;
+    if (tiles * (tokens > tile_tokens ? 2 : 1) > pa::kLeastCost) {  // (the bound on the rows: pa::schedule)
+        w.rows = 2ll * pa::kSegments * std::min(128ll, static_cast<long long>(tokens) * group);
+        w.plan = take(sizeof(pa::Plan) * static_cast<unsigned long long>(c->sequences));
+        w.stats = take(8ull * w.rows);
+        w.o = take(4ull * w.rows * c->d);
+    }
     return w;
+}
+
+template <int D>
+int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, char* workspace, const PagedWorkspace& w,
+                 int tokens, int heads, float scale, int sm_count, cudaStream_t stream) {
+    using L = pa::Smem<D>;
+    const int group = heads / c->kv_heads, tile_tokens = 128 / group;
+    CUtensorMap tm_q, tm_k, tm_v;
+    // [tokens, key heads, heads of the group, d]; a dimension of size 1 gets a stride that the encoder accepts
+    const unsigned long long head = heads > 1 ? q_strides[1] : D, token = tokens > 1 ? q_strides[0] : D;
+    int rc = encode_4d(&tm_q, Q, D, group, c->kv_heads, tokens, 2 * head, 2 * head * group, 2 * token, 64, group, 1, tile_tokens);
+    const int box = std::min(c->page, kTile);
+    const uint64_t places = static_cast<uint64_t>(c->pages) * c->kv_heads;
+    if (rc == ATTNW_OK) rc = encode_3d(&tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c->K, D, c->page, places, 64, box);
+    if (rc == ATTNW_OK) rc = encode_3d(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c->V, D, c->page, places, 64, box);
+    if (rc != ATTNW_OK) return rc;
+    if (allow_smem<pa::attn_paged_kernel<D>>(L::kDynamicBytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    const paged::Cache view = view_of(c);
+    const pa::Shape shape{tokens, heads, group, tile_tokens, static_cast<int>(w.rows)};
+    const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(std::min(c->sequences, tokens))) * c->kv_heads;
+    const long long grid = blocks + (w.rows > 0 ? pa::kSegments : 0);
+    if (grid > INT_MAX) return ATTNW_ERR_BAD_SHAPE;
+    auto* plan = w.rows > 0 ? reinterpret_cast<pa::Plan*>(workspace + w.plan) : nullptr;
+    auto* stats = w.rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
+    auto* part = w.rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
+    const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
+    auto* o = static_cast<__nv_bfloat16*>(O);
+    cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(grid), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
+                                      shape, starts, scale_log2e, o, lse, part, stats, plan);
+    if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (e == cudaSuccess && plan) {
+        const long long rows = (static_cast<long long>(tokens) * heads + pa::kJoinWarps - 1) / pa::kJoinWarps;
+        e = launch_overlapped(pa::combine_kernel<D>, static_cast<unsigned>(std::min(rows, 8ll * sm_count)), pa::kJoinWarps * 32, 0, stream, 1, view, shape, starts,
+                              part, stats, plan, o, lse);
+        if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ATTNW_ERR_CUDA;
+    }
+    return ATTNW_OK;
 }
 
 int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
@@ -220,7 +277,7 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     if (rc != ATTNW_OK) return rc;
     if (!aligned16(Q) || !aligned16(O) || !aligned4(starts) || !aligned4(lse) || !aligned4(mass) || !aligned4(mass_out)) return ATTNW_ERR_MISALIGNED;
     const unsigned long long capacity = static_cast<unsigned long long>(c->table_width) * c->page, weights = 4ull * c->sequences * c->kv_heads * capacity;
-    const PagedWorkspace w = paged_workspace(c, tokens, heads, mass != nullptr, lse != nullptr);
+    const PagedWorkspace w = paged_workspace(c, tokens, heads, mass != nullptr);
     if (w.bytes > 0 && !workspace) return ATTNW_ERR_NULL_POINTER;
     if (workspace_bytes < w.bytes) return ATTNW_ERR_BAD_SHAPE;
     if (w.bytes > 0 && !aligned16(workspace)) return ATTNW_ERR_MISALIGNED;
@@ -237,25 +294,21 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     DeviceInfo* dev = nullptr;
     rc = current_device(&dev);
     if (rc != ATTNW_OK) return rc;
-    const paged::Cache view = view_of(c);
+    rc = load_encoder();
+    if (rc != ATTNW_OK) return rc;
     float* own_lse = lse ? lse : mass ? reinterpret_cast<float*>(static_cast<char*>(workspace) + w.lse) : nullptr;
-    const auto* q = static_cast<const __nv_bfloat16*>(Q);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const long long warps = static_cast<long long>(tokens) * heads;
-    cudaError_t e = launch_overlapped_3d(c->d == 64 ? pa0::attn_kernel<64> : pa0::attn_kernel<128>, static_cast<unsigned>((warps + pa0::kWarps - 1) / pa0::kWarps),
-                                         1, 1, pa0::kWarps * 32, s, q, q_strides[0], q_strides[1], view, starts, static_cast<__nv_bfloat16*>(O), own_lse,
-                                         tokens, heads, scale);
-    if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (e == cudaSuccess && mass) {
-        e = launch_overlapped_3d(c->d == 64 ? pa0::mass_kernel<64> : pa0::mass_kernel<128>, static_cast<unsigned>((capacity + 127) / 128),
-                                 static_cast<unsigned>(c->sequences * c->kv_heads), 1, 128, s, q, q_strides[0], q_strides[1], view, starts, own_lse, mass,
-                                 mass_out, tokens, heads, scale, static_cast<int>(capacity));
-        if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
-    }
-    if (e != cudaSuccess) {
+    const auto launch = c->d == 64 ? launch_paged<64> : launch_paged<128>;
+    rc = launch(c, Q, q_strides, starts, O, own_lse, static_cast<char*>(workspace), w, tokens, heads, scale, dev->sm_count, s);
+    if (rc != ATTNW_OK || !mass) return rc;
+    const auto* q = static_cast<const __nv_bfloat16*>(Q);
+    if (launch_overlapped_3d(c->d == 64 ? pm::mass_kernel<64> : pm::mass_kernel<128>, static_cast<unsigned>((capacity + 127) / 128),
+                             static_cast<unsigned>(c->sequences * c->kv_heads), 1, 128, s, q, q_strides[0], q_strides[1], view_of(c), starts, own_lse, mass,
+                             mass_out, tokens, heads, scale, static_cast<int>(capacity)) != cudaSuccess) {
         (void)cudaGetLastError();
         return ATTNW_ERR_CUDA;
     }
+    g_launches.fetch_add(1, std::memory_order_relaxed);
     return ATTNW_OK;
 }
 

@@ -226,6 +226,11 @@ ATTENTION = [
     (12, 4, 64, 32, [(300, 301), (1, 900), (17, 18), (0, 3), (256, 512)]),
     (2, 2, 128, 16, [(513, 1030)]),
     (4, 2, 64, 64, [(3, 0), (2, 1), (1, 0)]),
+    # many key tiles a segment: the ring of tiles goes round, split blocks (also with heads of 64) and whole ones
+    (16, 8, 128, 64, [(1, 9000 + 100 * i) for i in range(8)]),
+    (16, 8, 64, 64, [(1, 9000 + 100 * i) for i in range(8)]),
+    (8, 1, 128, 128, [(300, 8500)]),
+    (32, 8, 64, 32, [(300, 5000), (33, 5100)]),
 ]
 
 
