@@ -107,6 +107,24 @@ struct Smem {
 };
 static_assert(Smem<128>::kDynamicBytes <= 227 * 1024, "shared memory budget");
 
+// The stages that the tiles of a kind (K 0, V 1) go through, and the parity of the stage's use.  Two issuers: each kind has stages of its
+// own, since an issuer waits by parity for its own kind alone and would take the use before the last for the last where the one between is the
+// other's and has not arrived (possible as soon as tiles come from HBM).  One issuer: it waits for all, which share the stages.
+template <int STAGES, bool TWO_ISSUERS>
+struct Tiles {
+    static constexpr int kK = TWO_ISSUERS ? STAGES / 2 : STAGES;  // (V tiles stay longer)
+    int stage, first, behind;
+    uint32_t parity = 0;
+    __host__ __device__ __forceinline__ explicit Tiles(int kind)
+        : stage(TWO_ISSUERS && kind == 1 ? kK : 0), first(stage), behind(TWO_ISSUERS && kind == 0 ? kK : STAGES) {}
+    __host__ __device__ __forceinline__ void next() {
+        if (++stage == behind) {
+            stage = first;
+            parity ^= 1u;
+        }
+    }
+};
+
 struct Barriers {
     uint64_t q_full;
     uint64_t k_full[7], k_empty[7];
@@ -215,7 +233,8 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = bars->tmem_base;
-    int loads = 0;  // producer: ring entries asked for
+    using Ring = Tiles<kStages, two_issuers>;
+    int loads[2] = {0, 0};  // producer: tiles asked for, of each kind (one issuer: all in the first)
 
     if (warp == kProducer) {
         // ================= TMA producer: Q once, then the K and V tiles in the order the MMA issuer reads them =========
@@ -234,12 +253,13 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                                          row0 + q * kTile, bh, keep);
             }
             if (whole_warp) __syncwarp();
-            int n = 0;
+            Ring k_tiles(0), v_tiles(1);
+            int k_count = 0, v_count = 0;
             bool ok = true;
-            auto load = [&](const CUtensorMap* map, int kt) {
+            auto load = [&](const CUtensorMap* map, int kt, Ring& tiles, int& count) {
                 if (!ok) return;
-                const int s = n % kStages;
-                const uint32_t parity = (static_cast<uint32_t>(n / kStages) & 1u) ^ 1u;
+                const int s = tiles.stage;
+                const uint32_t parity = tiles.parity ^ 1u;
                 ok = whole_warp ? warp_wait(bar_of(offsetof(Barriers, k_empty), s), parity, abort_flag, kSiteProducerEmpty)
                                 : fused_wait(&bars->k_empty[s], parity, abort_flag, kSiteProducerEmpty);
                 if (!ok) return;
@@ -249,16 +269,18 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         ptx::tma_load_3d(smem + stage_offset(s) + a * L::kAtomBytes, map, &bars->k_full[s], a * 64, kt * kTile, bh, keep);
                 }
                 if (whole_warp) __syncwarp();
-                ++n;
+                tiles.next();
+                ++count;
             };
             const int lists = split ? 2 : 1;  // units that have key tiles of their own
             for (int j = -1; ok && j < steps[0]; ++j) {
                 for (int q = 0; q < lists; ++q) {
-                    if (j + 1 < steps[q]) load(&tm_k, key_tile(j + 1, q));
-                    if (j >= 0 && j < steps[q]) load(&tm_v, key_tile(j, q));
+                    if (j + 1 < steps[q]) load(&tm_k, key_tile(j + 1, q), k_tiles, k_count);
+                    if (j >= 0 && j < steps[q]) load(&tm_v, key_tile(j, q), two_issuers ? v_tiles : k_tiles, two_issuers ? v_count : k_count);
                 }
             }
-            loads = n;
+            loads[0] = k_count;
+            loads[1] = v_count;
         }
         __syncwarp();
     } else if (warp == kMma || (two_issuers && warp == kMmaProduct)) {
@@ -275,14 +297,13 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             ok = false;
             if constexpr (M == kCluster) tell_peers(&bars->abort_flag, G);
         }
-        int n = 0;            // next ring entry, in step with the producer
-        auto arrived = [&]() {
-            ok = ok && warp_wait(bar_of(offsetof(Barriers, k_full), n % kStages), static_cast<uint32_t>(n / kStages) & 1u, abort_flag, kSiteMmaKFull);
-        };
+        // The next tile: of the issuer's own kind where there are two; a single one has all, and takes the next two in an order of its own.
+        Ring tile(two_issuers && warp == kMmaProduct ? 1 : 0);
+        auto arrived = [&]() { ok = ok && warp_wait(bar_of(offsetof(Barriers, k_full), tile.stage), tile.parity, abort_flag, kSiteMmaKFull); };
         auto release = [&]() {  // the entry may be replaced once the MMAs issued so far are complete
-            if (ptx::elect_one()) ptx::umma_commit(&bars->k_empty[n % kStages]);
+            if (ptx::elect_one()) ptx::umma_commit(&bars->k_empty[tile.stage]);
             __syncwarp();
-            ++n;
+            tile.next();
         };
         int last_q = 0, last_j = -1;  // kSharedS: whose scores the buffer holds
         auto scores = [&](int q, int j) {  // S of step j
@@ -296,7 +317,7 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const uint32_t d_tmem = tmem_base + L::s_col(q);
             // (descriptors: the first of the tile plus a distance in 16-byte units)
             const uint64_t a_desc = ptx::umma_desc_kmajor_sw128(base + L::kQOff + (split ? 0u : static_cast<uint32_t>(q * L::kTileBytes)));
-            const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(stage_offset(n % kStages)));
+            const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(stage_offset(tile.stage)));
             if (ptx::elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
@@ -312,7 +333,7 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (!ok) return;
             ptx::tc_fence_after_sync();
             const uint32_t o_tmem = tmem_base + L::o_col(q), p_tmem = tmem_base + L::p_col(q);
-            const uint64_t b_desc = av::umma_desc_mnmajor_sw128(base + static_cast<uint32_t>(stage_offset(n % kStages)), L::kAtomBytes);
+            const uint64_t b_desc = av::umma_desc_mnmajor_sw128(base + static_cast<uint32_t>(stage_offset(tile.stage)), L::kAtomBytes);
             if (ptx::elect_one()) {
 #pragma unroll
                 for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per instruction
@@ -337,8 +358,6 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             scores(q, j + 1);
                             if (!split && steps[1] > 0) scores(1, j + 1);
                             release();
-                        } else {
-                            ++n;
                         }
                     }
                     if (j >= 0 && j < steps[q]) {  // V of step j
@@ -347,8 +366,6 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                             product(q, j);
                             if (!split && steps[1] > 0) product(1, j);
                             release();
-                        } else {
-                            ++n;
                         }
                     }
                 }
@@ -357,23 +374,26 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             static_assert(two_issuers || !split, "one issuer: two query tiles");
             for (int j = -1; ok && j < steps[0]; ++j) {
                 const bool next = j + 1 < T;
-                const int k_entry = n, v_entry = next ? n + 1 : n;  // K of step j + 1, V of step j
+                const Ring k_tile = tile;  // K of step j + 1, V of step j
+                if (next) tile.next();
+                const Ring v_tile = tile;
+                tile = k_tile;
                 if (next) {
                     arrived();
                     scores(0, j + 1);
                 }
-                n = v_entry;
+                tile = v_tile;
                 if (ok && j >= 0) {
                     arrived();
                     product(0, j);
                 }
                 if (ok && next) {
-                    n = k_entry;
+                    tile = k_tile;
                     if (steps[1] > 0) scores(1, j + 1);
                     release();
                 }
                 if (ok && j >= 0) {
-                    n = v_entry;
+                    tile = v_tile;
                     if (steps[1] > 0) product(1, j);
                     release();
                 }
@@ -710,10 +730,12 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         // Unwinding: let the copies already in flight land before shared memory is released.
         if (warp == kProducer && lane == 0) {
             const long long t0 = clock64();
-            for (int it = loads > kStages ? loads - kStages : 0; it < loads; ++it)
-                while (!ptx::mbar_try_wait(&bars->k_full[it % kStages], static_cast<uint32_t>(it / kStages) & 1u) &&
-                       clock64() - t0 < kWaitLimitCycles / 8) {
-                }
+            for (int kind = 0; kind < 2; ++kind) {
+                Ring tile(kind);
+                for (int it = 0; it < loads[kind]; ++it, tile.next())
+                    while (it + kStages >= loads[kind] && !ptx::mbar_try_wait(&bars->k_full[tile.stage], tile.parity) && clock64() - t0 < kWaitLimitCycles / 8) {
+                    }
+            }
             while (!ptx::mbar_try_wait(&bars->q_full, 0) && clock64() - t0 < kWaitLimitCycles / 8) {
             }
         }
