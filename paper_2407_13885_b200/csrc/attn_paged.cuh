@@ -56,8 +56,8 @@ struct Smem {
     // K and V tiles.  Split: one more, in the second query tile's place.  Each kind has a ring of its own, because it has an issuer of its own: an issuer
     // waits for its tiles by the parity of a stage's uses, and would take the use before the last for the last where the one between is the other's.
     static constexpr int kStages = (D == 128) ? 4 : 6;
-    static __device__ __forceinline__ int k_stages(bool whole) { return whole ? kStages / 2 : kStages / 2 + 1; }
-    static constexpr int kVStages = kStages / 2;
+    static constexpr int kKStages = kStages / 2;
+    static __device__ __forceinline__ int v_stages(bool whole) { return whole ? kStages / 2 : kStages / 2 + 1; }
     // Tensor memory as in attn_onepass.cuh: d = 64 has room for scores, O and P of both units, d = 128 for one buffer of scores that they use in turn.
     static constexpr bool kSharedS = D == 128;
     static __host__ __device__ constexpr uint32_t s_col(int q) { return kSharedS ? 0u : static_cast<uint32_t>(q * 256); }
@@ -88,7 +88,7 @@ struct Segment {
 
 struct Barriers {
     uint64_t q_full;
-    uint64_t k_full[4], k_empty[4], v_full[3], v_empty[3];
+    uint64_t k_full[3], k_empty[3], v_full[4], v_empty[4];
     uint64_t s_full[2], s_free[2];  // per unit: scores written / read into registers (8 warps)
     uint64_t p_full[2], p_free[2];  // per unit: P written (8 warps) / read by its MMAs
     uint64_t o_full[2];             // per unit: every product complete
@@ -217,11 +217,11 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     // ---- set-up ------------------------------------------------------------------------------
     if (warp == kProducer && lane == 0) {
         ptx::mbar_init(&bars->q_full, 1);
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 3; ++s) {
             ptx::mbar_init(&bars->k_full[s], 1);
             ptx::mbar_init(&bars->k_empty[s], 1);
         }
-        for (int s = 0; s < 3; ++s) {
+        for (int s = 0; s < 4; ++s) {
             ptx::mbar_init(&bars->v_full[s], 1);
             ptx::mbar_init(&bars->v_empty[s], 1);
         }
@@ -256,9 +256,9 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     // The key tiles of a unit: all of them, or every other one.
     const int steps[2] = {whole ? tiles : (tiles + 1) / 2, whole ? tiles : tiles / 2};
     const int tile0 = seg.tile0;
-    const int k_stages = L::k_stages(whole);
-    auto v_offset = [](int s) { return L::kKOff + s * L::kTileBytes; };
-    auto k_offset = [](int s) { return s < L::kStages - L::kVStages ? L::kKOff + (L::kVStages + s) * L::kTileBytes : L::kQOff + L::kTileBytes; };
+    const int v_stages = L::v_stages(whole);
+    auto k_offset = [](int s) { return L::kKOff + s * L::kTileBytes; };
+    auto v_offset = [](int s) { return s < L::kStages - L::kKStages ? L::kKOff + (L::kKStages + s) * L::kTileBytes : L::kQOff + L::kTileBytes; };
     auto key_tile = [&](int j, int q) { return tile0 + (whole ? j : 2 * j + q); };
     struct Entry {  // of a ring
         int stage = 0;
@@ -313,12 +313,12 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         };
         auto load_k = [&](int kt, int where) {
             load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), bar_of(offsetof(Barriers, k_empty), ek.stage), ek.phase, smem + k_offset(ek.stage), kt, where);
-            ek.next(k_stages);
+            ek.next(L::kKStages);
             k_loads += ok ? 1 : 0;
         };
         auto load_v = [&](int kt, int where) {
             load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), bar_of(offsetof(Barriers, v_empty), ev.stage), ev.phase, smem + v_offset(ev.stage), kt, where);
-            ev.next(L::kVStages);
+            ev.next(v_stages);
             v_loads += ok ? 1 : 0;
         };
         const int lists = whole ? 1 : 2;  // units that have key tiles of their own
@@ -405,7 +405,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     arrived(offsetof(Barriers, k_full));
                     scores(q, j);
                     if (whole) scores(1, j);
-                    release(bars->k_empty, k_stages);
+                    release(bars->k_empty, L::kKStages);
                 }
             }
         } else {
@@ -416,7 +416,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     clear_unused(key_tile(j, q));
                     product(q, j);
                     if (whole) product(1, j);
-                    release(bars->v_empty, L::kVStages);
+                    release(bars->v_empty, v_stages);
                 }
             }
         }
@@ -665,8 +665,8 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     while (!ptx::mbar_try_wait(&full[it % stages], static_cast<uint32_t>(it / stages) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
                     }
             };
-            land(bars->k_full, k_stages, k_loads);
-            land(bars->v_full, L::kVStages, v_loads);
+            land(bars->k_full, L::kKStages, k_loads);
+            land(bars->v_full, v_stages, v_loads);
             while (!ptx::mbar_try_wait(&bars->q_full, 0) && clock64() - t0 < kWaitLimitCycles / 8) {
             }
         }
