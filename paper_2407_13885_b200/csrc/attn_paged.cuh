@@ -83,6 +83,7 @@ struct Segment {
     int tile0, tile1;  // key tiles
     int segments;      // that the block is cut into
     int whole;
+    int q_tile;        // the block's first query tile, among those of all sequences
     long long part;    // segments > 1: the workspace's row of the segment's first row
 };
 
@@ -103,6 +104,7 @@ struct Shape {
     int tokens, heads, group;  // query heads of a key head
     int tile_tokens;           // tokens of a query tile: floor(128 / group)
     int part_rows;             // rows that the workspace has
+    int q_tiles;               // query tiles a key head, at most (of all sequences)
 };
 
 // A sequence's part in the schedule.
@@ -139,11 +141,15 @@ __device__ __forceinline__ long long warp_scan(long long x, int lane) {  // incl
     return x;
 }
 
-// What combine_kernel has to know of a sequence: the segments of its blocks (1: nothing to join) and the workspace's row that they begin at.
+// What combine_kernel has to know of a sequence: the segments of its blocks (1: nothing to join), the workspace's row that they begin at, and the
+// first of its query tiles.
 struct Plan {
     int segments, rows;
-    long long part;
+    long long part, q_tile;
 };
+
+// Where the sums of a query tile's rows lie for mass_kernel: minus their logarithms to base 2, float [query tile][key head][128].
+__device__ __forceinline__ size_t lse2_row(const paged::Cache& c, long long q_tile, int h) { return (static_cast<size_t>(q_tile) * c.kv_heads + h) * kTile; }
 
 // By one warp.  Finds segment `index`; index 0 also writes the plan.
 __device__ __noinline__ void schedule(const paged::Cache& c, const Shape& s, const int* starts, int index, Segment* out, Plan* plan) {
@@ -159,7 +165,7 @@ __device__ __noinline__ void schedule(const paged::Cache& c, const Shape& s, con
     // The cost of a segment; one of two query tiles twice that.  So there are at most kSegments more segments than blocks, and those that come
     // from cutting a block up are at most 2 kSegments, of 128 rows at most (or half as many, of 256).
     const long long most = max(static_cast<long long>(kLeastCost), (total + kSegments - 1) / kSegments);
-    long long first = 0, part = 0;  // segments and workspace rows of the sequences in front
+    long long first = 0, part = 0, q_first = 0;  // segments, workspace rows and query tiles of the sequences in front
     if (lane == 0) out->b = -1;
     __syncwarp();
     for (int b0 = 0; b0 < c.sequences; b0 += 32) {
@@ -173,7 +179,8 @@ __device__ __noinline__ void schedule(const paged::Cache& c, const Shape& s, con
         const long long part_end = part + warp_scan(rows, lane);
         if (part_end > s.part_rows) cut = 1;  // (the host's bound holds for tokens that belong to one sequence each)
         const long long end = first + warp_scan(blocks * cut, lane), begin = end - blocks * cut;
-        if (index == 0 && plan && b < c.sequences) plan[b] = {cut, r.rows, part_end - rows};
+        const long long q_tiles = (r.n + s.tile_tokens - 1) / s.tile_tokens, q_end = q_first + warp_scan(q_tiles, lane);
+        if (index == 0 && plan && b < c.sequences) plan[b] = {cut, r.rows, part_end - rows, q_end - q_tiles};
         if (index >= begin && index < end) {
             int at = static_cast<int>(index - begin);
             const int seg = at % cut;
@@ -190,20 +197,30 @@ __device__ __noinline__ void schedule(const paged::Cache& c, const Shape& s, con
             out->tile1 = static_cast<int>(static_cast<long long>(tiles) * (seg + 1) / cut);
             out->segments = cut;
             out->whole = out->tokens > s.tile_tokens;
+            out->q_tile = static_cast<int>(q_end - q_tiles) + 2 * block;
             out->part = part_end - rows + ((static_cast<long long>(block) * c.kv_heads + h) * cut + seg) * r.rows;
             out->b = b;
         }
         first = __shfl_sync(0xffffffffu, end, 31);
         part = __shfl_sync(0xffffffffu, part_end, 31);
+        q_first = __shfl_sync(0xffffffffu, q_end, 31);
     }
     __syncwarp();
+}
+
+// The logarithm of a row's sum l 2^top: to the caller, and for mass_kernel.
+__device__ __forceinline__ void store_lse(const paged::Cache& c, const Shape& s, float* lse, float* lse2, size_t out_row, long long q_tile, int h, int row, float top,
+                                          float l) {
+    const float log2_sum = l > 0.0f ? top + ptx::lg2_approx(l) : __int_as_float(0xff800000);
+    if (lse) lse[out_row] = 0.69314718055994531f * log2_sum;
+    if (lse2 && q_tile < s.q_tiles) lse2[lse2_row(c, q_tile, h) + row] = -log2_sum;  // (the host's bound holds for tokens of one sequence each)
 }
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, float scale_log2e,
-                  __nv_bfloat16* O, float* lse, float* part_o, float2* part_stats, Plan* plan) {
+                  __nv_bfloat16* O, float* lse, float* lse2, float* part_o, float2* part_stats, Plan* plan) {
     using L = Smem<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -612,8 +629,8 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             if (stored && half == 0 && (whole || q == 0)) {
                 if (joined)
                     part_stats[part_row] = make_float2(top, l_row);
-                else if (lse)
-                    lse[out_row] = l_row > 0.0f ? 0.69314718055994531f * (top + ptx::lg2_approx(l_row)) : __int_as_float(0xff800000);
+                else
+                    store_lse(cache, shape, lse, lse2, out_row, seg.q_tile + (whole ? q : 0), seg.h, row, top, l_row);
             }
             __syncwarp();
             const uint32_t o_unit = t_quarter + L::o_col(q), o_peer = t_quarter + L::o_col(q ^ 1);
@@ -683,7 +700,7 @@ constexpr int kJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, const float* part_o, const float2* part_stats,
-               const Plan* plan, __nv_bfloat16* O, float* lse) {
+               const Plan* plan, __nv_bfloat16* O, float* lse, float* lse2) {
     __shared__ paged::Samples samples;
     ptx::grid_dependency_wait();
     if (*reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u) return;
@@ -719,7 +736,8 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
         __nv_bfloat16* dst = O + static_cast<size_t>(id) * D + lane * kCols;
 #pragma unroll
         for (int c = 0; c < kCols; c += 2) *reinterpret_cast<uint32_t*>(dst + c) = ptx::pack_bf16x2(v[c] * inv, v[c + 1] * inv);
-        if (lse && lane == 0) lse[id] = l > 0.0f ? 0.69314718055994531f * (top + ptx::lg2_approx(l)) : __int_as_float(0xff800000);
+        if (lane == 0)
+            store_lse(cache, shape, lse, lse2, static_cast<size_t>(id), p.q_tile + i / shape.tile_tokens, h, i % shape.tile_tokens * shape.group + g, top, l);
     }
 }
 

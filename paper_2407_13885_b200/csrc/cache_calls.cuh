@@ -197,7 +197,8 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
 
 // Where the parts of attn_paged's workspace begin.
 struct PagedWorkspace {
-    unsigned long long lse = 0, plan = 0, stats = 0, o = 0, bytes = 0;
+    unsigned long long lse2 = 0, plan = 0, stats = 0, o = 0, bytes = 0;
+    int q_tiles = 0;
     long long rows = 0;  // of the segments' parts; 0: no block is long enough to be cut
 };
 PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool weigh) {
@@ -207,8 +208,9 @@ PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool
         w.bytes = (w.bytes + bytes + 255) / 256 * 256;
         return at;
     };
-    if (weigh) w.lse = take(4ull * tokens * heads);
     const int group = heads / c->kv_heads, tile_tokens = 128 / group;
+    w.q_tiles = tokens / tile_tokens + std::min(c->sequences, tokens);
+    if (weigh) w.lse2 = take(4ull * kTile * w.q_tiles * c->kv_heads);
     const long long tiles = (static_cast<long long>(c->table_width) * c->page + kTile - 1) / kTile;
     if (tiles * (tokens > tile_tokens ? 2 : 1) > pa::kLeastCost) {  // (the bound on the rows: pa::schedule)
         w.rows = 2ll * pa::kSegments * std::min(128ll, static_cast<long long>(tokens) * group);
@@ -220,8 +222,8 @@ PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool
 }
 
 template <int D>
-int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, char* workspace, const PagedWorkspace& w,
-                 int tokens, int heads, float scale, int sm_count, cudaStream_t stream) {
+int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
+                 char* workspace, const PagedWorkspace& w, int tokens, int heads, float scale, int sm_count, cudaStream_t stream) {
     using L = pa::Smem<D>;
     const int group = heads / c->kv_heads, tile_tokens = 128 / group;
     CUtensorMap tm_q, tm_k, tm_v;
@@ -238,7 +240,7 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
         return ATTNW_ERR_CUDA;
     }
     const paged::Cache view = view_of(c);
-    const pa::Shape shape{tokens, heads, group, tile_tokens, static_cast<int>(w.rows)};
+    const pa::Shape shape{tokens, heads, group, tile_tokens, static_cast<int>(w.rows), w.q_tiles};
     const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(std::min(c->sequences, tokens))) * c->kv_heads;
     const long long grid = blocks + (w.rows > 0 ? pa::kSegments : 0);
     if (grid > INT_MAX) return ATTNW_ERR_BAD_SHAPE;
@@ -247,13 +249,23 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
     auto* part = w.rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
     const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
     auto* o = static_cast<__nv_bfloat16*>(O);
+    auto* lse2 = mass ? reinterpret_cast<float*>(workspace + w.lse2) : nullptr;
     cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(grid), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
-                                      shape, starts, scale_log2e, o, lse, part, stats, plan);
+                                      shape, starts, scale_log2e, o, lse, lse2, part, stats, plan);
     if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && plan) {
         const long long rows = (static_cast<long long>(tokens) * heads + pa::kJoinWarps - 1) / pa::kJoinWarps;
         e = launch_overlapped(pa::combine_kernel<D>, static_cast<unsigned>(std::min(rows, 8ll * sm_count)), pa::kJoinWarps * 32, 0, stream, 1, view, shape, starts,
-                              part, stats, plan, o, lse);
+                              part, stats, plan, o, lse, lse2);
+        if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    if (e == cudaSuccess && mass) {
+        // segments: at most kSegments more than one a (sequence with new tokens, key head)
+        const long long segments = pm::kSegments + static_cast<long long>(std::min(c->sequences, tokens)) * c->kv_heads;
+        e = allow_smem<pm::mass_kernel<D>>(pm::Smem<D>::kDynamicBytes);
+        if (e == cudaSuccess)
+            e = launch_overlapped(pm::mass_kernel<D>, static_cast<unsigned>(segments), pm::kThreads, pm::Smem<D>::kDynamicBytes, stream, 1, tm_q, tm_k, view, shape,
+                                  starts, lse2, scale_log2e, mass, mass_out);
         if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     if (e != cudaSuccess) {
@@ -296,20 +308,9 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     if (rc != ATTNW_OK) return rc;
     rc = load_encoder();
     if (rc != ATTNW_OK) return rc;
-    float* own_lse = lse ? lse : mass ? reinterpret_cast<float*>(static_cast<char*>(workspace) + w.lse) : nullptr;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const auto launch = c->d == 64 ? launch_paged<64> : launch_paged<128>;
-    rc = launch(c, Q, q_strides, starts, O, own_lse, static_cast<char*>(workspace), w, tokens, heads, scale, dev->sm_count, s);
-    if (rc != ATTNW_OK || !mass) return rc;
-    const auto* q = static_cast<const __nv_bfloat16*>(Q);
-    if (launch_overlapped_3d(c->d == 64 ? pm::mass_kernel<64> : pm::mass_kernel<128>, static_cast<unsigned>((capacity + 127) / 128),
-                             static_cast<unsigned>(c->sequences * c->kv_heads), 1, 128, s, q, q_strides[0], q_strides[1], view_of(c), starts, own_lse, mass,
-                             mass_out, tokens, heads, scale, static_cast<int>(capacity)) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return ATTNW_ERR_CUDA;
-    }
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return ATTNW_OK;
+    return launch(c, Q, q_strides, starts, O, lse, mass, mass_out, static_cast<char*>(workspace), w, tokens, heads, scale, dev->sm_count,
+                  static_cast<cudaStream_t>(stream));
 }
 
 int evict_entry(const attnw_cache* c, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out, int budget,
