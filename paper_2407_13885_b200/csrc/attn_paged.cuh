@@ -9,11 +9,12 @@
 // one (sequence, key head).  Its CTA has two units that share the tensor pipe:
 //   whole   two query tiles: unit q has tile q, every key tile serves both;
 //   split   one query tile (decoding, and what a chunk leaves over): unit 0 has the even key tiles, unit 1 the odd ones, merged at the end.
-// A key tile is 128 keys of one or more pages, one TMA box (per 64 features) a page.  The keys of a block may be cut into segments, each a CTA's:
-// its unnormalised O, offset and sum go to a workspace and combine_kernel joins them.
+// A key tile is 128 keys of one or more pages, one TMA box (per 64 features) a page.
 //
-// What the host knows is the number of tokens, of sequences, and the width of the table; the lengths are on the device.  So each CTA works out for itself
-// what it does (schedule): the cost of all blocks, the segment length that gives kSegments of them, and which segment has its index.
+// What the host knows is the number of tokens, of sequences, and the width of the table; the lengths are on the device.  So there is one CTA an SM,
+// and each works out for itself what it does: all blocks lie in a row, each as long as it costs, and the CTA has a stretch of it (Walk).  It may
+// begin and end inside a block: then its unnormalised O, offset and sum go to a workspace, and combine_kernel joins them.  A CTA
+// goes through its blocks without a stop: while its Softmax warps finish one, the tiles of the next arrive.
 #pragma once
 #include <cstddef>
 
@@ -26,13 +27,18 @@ namespace pa {
 using av1::kLazy;
 using av1::kPassAt;
 
-constexpr int kThreads = 608;
+constexpr int kThreads = 640;
 constexpr int kSmWarps = 16;  // Softmax warps: unit (2) x column half (2) x TMEM lane quarter (4)
 constexpr int kProducer = 16;
 constexpr int kMma = 17;         // the scores' issuer
 constexpr int kMmaProduct = 18;  // the products'
-constexpr int kSegments = 592;   // about as many segments are wanted in all: four an SM of a B200
-constexpr int kLeastCost = 4;    // of a segment: key tiles of one query tile
+constexpr int kScheduler = 19;
+constexpr int kRoles = 19;       // warps that work on segments
+// Costs are in keys of one query tile (two query tiles: twice that).
+constexpr int kBlockCost = 2 * kTile;                // of a block besides: its set-up and its result
+constexpr int kLeastCost = kBlockCost + 4 * kTile;   // of a CTA's stretch
+constexpr int kLeastCut = 8;                         // key tiles of a block that may be cut
+constexpr int kSlots = 4;                            // segments on their way from the scheduler to the others
 
 enum : uint32_t {  // wait sites of this kernel (low byte of the status word)
     kSiteProducerEmpty = 112,
@@ -44,6 +50,10 @@ enum : uint32_t {  // wait sites of this kernel (low byte of the status word)
     kSitePFree = 118,
     kSiteOFull = 119,
     kSiteLFull = 120,
+    kSiteOFree = 121,
+    kSiteQFree = 122,
+    kSiteSegment = 123,
+    kSiteSegmentFree = 124,
 };
 
 constexpr int kUnitStats = 4 * kTile;
@@ -53,64 +63,80 @@ struct Smem {
     static constexpr int kAtoms = D / 64;
     static constexpr int kAtomBytes = kTile * 128;          // 128 rows x 128 bytes
     static constexpr int kTileBytes = kAtoms * kAtomBytes;  // a Q, K or V tile
-    // K and V tiles.  Split: one more, in the second query tile's place.  Each kind has a ring of its own, because it has an issuer of its own: an issuer
-    // waits for its tiles by the parity of a stage's uses, and would take the use before the last for the last where the one between is the other's.
-    static constexpr int kStages = (D == 128) ? 4 : 6;
-    static constexpr int kKStages = kStages / 2;
-    static __device__ __forceinline__ int v_stages(bool whole) { return whole ? kStages / 2 : kStages / 2 + 1; }
+    // K and V tiles.  Each kind has a ring of its own, because it has an issuer of its own: an issuer waits for its tiles by the parity of a
+    // stage's uses, and would take the use before the last for the last where the one between is the other's.
+    static constexpr int kStages = (D == 128) ? 2 : 3;
     // Tensor memory as in attn_onepass.cuh: d = 64 has room for scores, O and P of both units, d = 128 for one buffer of scores that they use in turn.
     static constexpr bool kSharedS = D == 128;
     static __host__ __device__ constexpr uint32_t s_col(int q) { return kSharedS ? 0u : static_cast<uint32_t>(q * 256); }
     static __host__ __device__ constexpr uint32_t p_col(int q) { return kSharedS ? 128u + static_cast<uint32_t>(q * 64) : static_cast<uint32_t>(q * 256 + 192); }
     static __host__ __device__ constexpr uint32_t o_col(int q) { return kSharedS ? 256u + static_cast<uint32_t>(q * 128) : static_cast<uint32_t>(q * 256 + 128); }
     static constexpr int kQOff = 0;
-    static constexpr int kKOff = kQOff + 2 * kTileBytes;
-    static constexpr int kStatOff = kKOff + kStages * kTileBytes;  // per unit: maxima, float [2 steps][2 halves][128 rows]; at the end sums and offset
-    static constexpr int kBarOff = kStatOff + 2 * kUnitStats * 4;
-    static constexpr int kBytes = kBarOff + 512;
+    static constexpr int kKOff = kQOff + 2 * kTileBytes;  // (two query tiles: of one block, or of two split ones)
+    static constexpr int kVOff = kKOff + kStages * kTileBytes;
+    static constexpr int kStatOff = kVOff + kStages * kTileBytes;  // per unit: maxima, float [2 steps][2 halves][128 rows]
+    static constexpr int kSumOff = kStatOff + 2 * 4 * kTile * 4;    // per unit: sums of both halves, offset, float [3][128]
+    static constexpr int kBarOff = kSumOff + 2 * 3 * kTile * 4;
+    static constexpr int kBytes = kBarOff + 768;
     static constexpr int kDynamicBytes = kBytes + 1024;
 };
 static_assert(Smem<128>::kDynamicBytes <= 227 * 1024, "shared memory budget");
 
-// What one CTA does.
+// A block, or a part of its keys, that a CTA works on.
 struct Segment {
-    int b;             // sequence, -1: nothing
+    int b;             // sequence, -1: there is no more
     int h;             // key head
     int token0;        // the block's first token and how many it has
     int tokens;
     int seen0;         // keys that the first token sees, not cut off below zero
     int length;        // keys of the sequence
     int tile0, tile1;  // key tiles
-    int segments;      // that the block is cut into
     int whole;
     int q_tile;        // the block's first query tile, among those of all sequences
-    long long part;    // segments > 1: the workspace's row of the segment's first row
+    int part;          // the workspace's slot; -1: the segment is all of the block
 };
 
 struct Barriers {
-    uint64_t q_full;
-    uint64_t k_full[3], k_empty[3], v_full[4], v_empty[4];
+    uint64_t q_full[2], q_free[2];  // per query tile's place
+    uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3];
     uint64_t s_full[2], s_free[2];  // per unit: scores written / read into registers (8 warps)
     uint64_t p_full[2], p_free[2];  // per unit: P written (8 warps) / read by its MMAs
-    uint64_t o_full[2];             // per unit: every product complete
+    uint64_t o_full[2];             // per unit: every product of a segment complete
+    uint64_t o_free;                // split: O of both units has been read (16 warps)
     uint64_t l_full[2], l_both;     // the row statistics are in shared memory: whole, per unit (8 warps); split (16)
+    uint64_t seg_full[kSlots], seg_free[kSlots];
     uint32_t tmem_base;
     uint32_t abort_flag;
-    Segment segment;
+    Segment segment[kSlots];
 };
-static_assert(sizeof(Barriers) <= 512, "barrier block must fit its slot");
+static_assert(sizeof(Barriers) <= 768, "barrier block must fit its slot");
 
 struct Shape {
     int tokens, heads, group;  // query heads of a key head
     int tile_tokens;           // tokens of a query tile: floor(128 / group)
-    int part_rows;             // rows that the workspace has
+    int part_rows;             // rows of a slot of the workspace; 0: no block can be cut
     int q_tiles;               // query tiles a key head, at most (of all sequences)
+    int ctas;                  // of attn_paged_kernel
 };
 
-// A sequence's part in the schedule.
+// A sequence's blocks.
 struct Share {
-    int n, seen0, length, blocks, rows;  // new tokens, (see Segment), blocks a key head, rows of a block
-    long long cost;                      // of a block
+    int n, seen0, length, blocks;  // new tokens, (see Segment), blocks a key head
+
+    __device__ __forceinline__ int tokens_of(const Shape& s, int r) const { return min(n - r * 2 * s.tile_tokens, 2 * s.tile_tokens); }
+    __device__ __forceinline__ int seen_of(const Shape& s, int r) const {  // keys that block r's last token sees
+        return min(max(seen0 + r * 2 * s.tile_tokens + tokens_of(s, r) - 1, 0), length);
+    }
+    // Cost of the first r blocks.  All but the last have as many tokens, and each sees that many more keys than the one in front.
+    __device__ __forceinline__ long long cost_upto(const Shape& s, int r) const {
+        if (r == 0) return 0;
+        const long long step = 2 * s.tile_tokens, least = seen0 + step - 1;
+        const int even = min(r, blocks - 1);
+        const long long skip = least > 0 ? 0 : (step - least) / step, m = even - skip;  // blocks in front that see nothing
+        long long cost = static_cast<long long>(r) * kBlockCost + (m > 0 ? 2 * (m * (least + skip * step) + step * (m * (m - 1) / 2)) : 0);
+        if (r > even) cost += static_cast<long long>(seen_of(s, r - 1)) * (tokens_of(s, r - 1) > s.tile_tokens ? 2 : 1);
+        return cost;
+    }
 };
 
 __device__ __forceinline__ Share share_of(const paged::Cache& c, const Shape& s, const int* starts, int b) {
@@ -120,10 +146,8 @@ __device__ __forceinline__ Share share_of(const paged::Cache& c, const Shape& s,
     r.n = max(t1 - t0, 0);
     r.length = paged::length_of(c, b);
     const long long seen = static_cast<long long>(r.length) - (static_cast<long long>(s1) - t0) + 1;
-    r.seen0 = static_cast<int>(max(seen, -(1ll << 30)));
+    r.seen0 = static_cast<int>(min(max(seen, -(1ll << 30)), 1ll << 30));
     r.blocks = (r.n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens);
-    r.rows = min(r.n, 2 * s.tile_tokens) * s.group;
-    r.cost = static_cast<long long>((r.length + kTile - 1) / kTile) * (r.n > s.tile_tokens ? 2 : 1);
     return r;
 }
 
@@ -141,71 +165,123 @@ __device__ __forceinline__ long long warp_scan(long long x, int lane) {  // incl
     return x;
 }
 
-// What combine_kernel has to know of a sequence: the segments of its blocks (1: nothing to join), the workspace's row that they begin at, and the
-// first of its query tiles.
-struct Plan {
-    int segments, rows;
-    long long part, q_tile;
+// A warp's way along the row of all blocks: sequence by sequence, key head by key head, block by block.  Lane i has the share of sequence
+// b0 + i; everything else is the same in all lanes.
+struct Walk {
+    int lane, b0 = 0;
+    Share mine;
+    long long stretch;  // cost of a CTA's
+    // the block at hand
+    int b = -1, h = 0, r = 0, q_tile0 = 0;  // b < 0: behind the last
+    Share share;
+    long long begin = 0;
+
+    __device__ __forceinline__ void load(const paged::Cache& c, const Shape& s, const int* starts) {
+        mine = {};
+        if (b0 + lane < c.sequences) mine = share_of(c, s, starts, b0 + lane);
+    }
+    __device__ __forceinline__ void take(int from) {  // the share of lane `from`
+        share.n = __shfl_sync(0xffffffffu, mine.n, from);
+        share.seen0 = __shfl_sync(0xffffffffu, mine.seen0, from);
+        share.length = __shfl_sync(0xffffffffu, mine.length, from);
+        share.blocks = __shfl_sync(0xffffffffu, mine.blocks, from);
+    }
+    __device__ __forceinline__ int q_tiles_of(const Shape& s, const Share& x) const { return (x.n + s.tile_tokens - 1) / s.tile_tokens; }
+
+    // The cost of everything, and the block that `index` stretches behind the beginning lies in.
+    __device__ __forceinline__ void find(const paged::Cache& c, const Shape& s, const int* starts, long long index) {
+        lane = static_cast<int>(threadIdx.x & 31);
+        long long total = 0;
+        for (b0 = 0; b0 < c.sequences; b0 += 32) {
+            load(c, s, starts);
+            total += mine.cost_upto(s, mine.blocks) * c.kv_heads;
+        }
+        total = warp_sum(total);
+        stretch = max(static_cast<long long>(kLeastCost), (total + s.ctas - 1) / s.ctas);
+        const long long at = index * stretch;
+        long long first = 0;
+        int q_first = 0;
+        for (b0 = 0; b0 < c.sequences; b0 += 32) {
+            if (c.sequences > 32) load(c, s, starts);  // (else they are at hand)
+            const long long a_head = mine.cost_upto(s, mine.blocks), cost = a_head * c.kv_heads;
+            const long long end = first + warp_scan(cost, lane);
+            const int q_tiles = q_tiles_of(s, mine), q_end = q_first + static_cast<int>(warp_scan(q_tiles, lane));
+            const uint32_t here = __ballot_sync(0xffffffffu, at >= end - cost && at < end);
+            if (here) {
+                const int from = __ffs(here) - 1;
+                take(from);
+                b = b0 + from;
+                q_tile0 = __shfl_sync(0xffffffffu, q_end - q_tiles, from);
+                const long long seq_begin = __shfl_sync(0xffffffffu, end - cost, from), of_head = __shfl_sync(0xffffffffu, a_head, from);
+                h = static_cast<int>((at - seq_begin) / of_head);
+                begin = seq_begin + h * of_head;
+                int lo = 0, hi = share.blocks;  // cost_upto(lo) <= at - begin < cost_upto(hi)
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (share.cost_upto(s, mid) <= at - begin) lo = mid; else hi = mid;
+                }
+                r = lo;
+                begin += share.cost_upto(s, r);
+                return;
+            }
+            first = __shfl_sync(0xffffffffu, end, 31);
+            q_first = __shfl_sync(0xffffffffu, q_end, 31);
+        }
+    }
+    __device__ __forceinline__ void next(const paged::Cache& c, const Shape& s, const int* starts) {
+        begin += kBlockCost + static_cast<long long>(weight(s)) * share.seen_of(s, r);
+        if (++r < share.blocks) return;
+        r = 0;
+        if (++h < c.kv_heads) return;
+        h = 0;
+        q_tile0 += q_tiles_of(s, share);
+        int from = b - b0 + 1;
+        for (;;) {
+            const uint32_t left = from < 32 ? __ballot_sync(0xffffffffu, mine.blocks > 0) >> from << from : 0u;
+            if (left) {
+                from = __ffs(left) - 1;
+                take(from);
+                b = b0 + from;
+                return;
+            }
+            b0 += 32;
+            if (b0 >= c.sequences) {
+                b = -1;
+                return;
+            }
+            load(c, s, starts);
+            from = 0;
+        }
+    }
+    __device__ __forceinline__ int weight(const Shape& s) const { return share.tokens_of(s, r) > s.tile_tokens ? 2 : 1; }
+    __device__ __forceinline__ int tiles(const Shape& s) const { return (share.seen_of(s, r) + kTile - 1) / kTile; }
+    // How many of the block's key tiles lie in front of stretch `index`.
+    __device__ __forceinline__ int tiles_before(const Shape& s, long long index) const {
+        const int all = tiles(s), a_tile = weight(s) * kTile;
+        const long long into = index * stretch - begin - kBlockCost;
+        if (into <= 0) return 0;
+        const long long t = (into + a_tile - 1) / a_tile;
+        if (t >= all) return all;
+        if (all < kLeastCut) return 2 * t < all ? 0 : all;
+        const long long least = max(2ll, stretch / 32 / a_tile);  // a shorter part goes to the CTA with the rest
+        return t < least ? 0 : t > all - least ? all : static_cast<int>(t);
+    }
 };
 
 // Where the sums of a query tile's rows lie for mass_kernel: minus their logarithms to base 2, float [query tile][key head][128].
 __device__ __forceinline__ size_t lse2_row(const paged::Cache& c, long long q_tile, int h) { return (static_cast<size_t>(q_tile) * c.kv_heads + h) * kTile; }
 
-// By one warp.  Finds segment `index`; index 0 also writes the plan.
-__device__ __noinline__ void schedule(const paged::Cache& c, const Shape& s, const int* starts, int index, Segment* out, Plan* plan) {
-    const int lane = static_cast<int>(threadIdx.x & 31);
-    long long total = 0;
-    for (int b0 = 0; b0 < c.sequences; b0 += 32) {
-        if (b0 + lane < c.sequences) {
-            const Share r = share_of(c, s, starts, b0 + lane);
-            total += r.cost * r.blocks * c.kv_heads;
+// For a segment, or its place: not cut short when another wait has given up, because all roles then still go through all segments, and soon.
+__device__ __noinline__ bool segment_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t site) {
+    const long long t0 = clock64();
+    while (!__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) {
+        if (__any_sync(0xffffffffu, clock64() - t0 > 4 * kWaitLimitCycles)) {
+            *abort_flag = 1;
+            atomicCAS(&g_attnw_status, 0u, 0x80000000u | site);
+            return false;
         }
     }
-    total = warp_sum(total);
-    // The cost of a segment; one of two query tiles twice that.  So there are at most kSegments more segments than blocks, and those that come
-    // from cutting a block up are at most 2 kSegments, of 128 rows at most (or half as many, of 256).
-    const long long most = max(static_cast<long long>(kLeastCost), (total + kSegments - 1) / kSegments);
-    long long first = 0, part = 0, q_first = 0;  // segments, workspace rows and query tiles of the sequences in front
-    if (lane == 0) out->b = -1;
-    __syncwarp();
-    for (int b0 = 0; b0 < c.sequences; b0 += 32) {
-        const int b = b0 + lane;
-        Share r{};
-        if (b < c.sequences) r = share_of(c, s, starts, b);
-        const long long own_most = r.n > s.tile_tokens ? 2 * most : most;
-        int cut = static_cast<int>(max(1ll, (r.cost + own_most - 1) / own_most));
-        const long long blocks = static_cast<long long>(r.blocks) * c.kv_heads;
-        const long long rows = cut > 1 ? blocks * cut * r.rows : 0;
-        const long long part_end = part + warp_scan(rows, lane);
-        if (part_end > s.part_rows) cut = 1;  // (the host's bound holds for tokens that belong to one sequence each)
-        const long long end = first + warp_scan(blocks * cut, lane), begin = end - blocks * cut;
-        const long long q_tiles = (r.n + s.tile_tokens - 1) / s.tile_tokens, q_end = q_first + warp_scan(q_tiles, lane);
-        if (index == 0 && plan && b < c.sequences) plan[b] = {cut, r.rows, part_end - rows, q_end - q_tiles};
-        if (index >= begin && index < end) {
-            int at = static_cast<int>(index - begin);
-            const int seg = at % cut;
-            at /= cut;
-            const int h = at % c.kv_heads, block = r.blocks - 1 - at / c.kv_heads;  // the longest first
-            const int i0 = block * 2 * s.tile_tokens;
-            out->h = h;
-            out->token0 = min(max(starts[b], 0), s.tokens) + i0;
-            out->tokens = min(r.n - i0, 2 * s.tile_tokens);
-            out->seen0 = r.seen0 + i0;
-            out->length = r.length;
-            const int seen = min(max(out->seen0 + out->tokens - 1, 0), r.length), tiles = (seen + kTile - 1) / kTile;
-            out->tile0 = static_cast<int>(static_cast<long long>(tiles) * seg / cut);
-            out->tile1 = static_cast<int>(static_cast<long long>(tiles) * (seg + 1) / cut);
-            out->segments = cut;
-            out->whole = out->tokens > s.tile_tokens;
-            out->q_tile = static_cast<int>(q_end - q_tiles) + 2 * block;
-            out->part = part_end - rows + ((static_cast<long long>(block) * c.kv_heads + h) * cut + seg) * r.rows;
-            out->b = b;
-        }
-        first = __shfl_sync(0xffffffffu, end, 31);
-        part = __shfl_sync(0xffffffffu, part_end, 31);
-        q_first = __shfl_sync(0xffffffffu, q_end, 31);
-    }
-    __syncwarp();
+    return true;
 }
 
 // The logarithm of a row's sum l 2^top: to the caller, and for mass_kernel.
@@ -220,7 +296,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, float scale_log2e,
-                  __nv_bfloat16* O, float* lse, float* lse2, float* part_o, float2* part_stats, Plan* plan) {
+                  __nv_bfloat16* O, float* lse, float* lse2, float* part_o, float2* part_stats) {
     using L = Smem<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -233,16 +309,15 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 
     // ---- set-up ------------------------------------------------------------------------------
     if (warp == kProducer && lane == 0) {
-        ptx::mbar_init(&bars->q_full, 1);
         for (int s = 0; s < 3; ++s) {
             ptx::mbar_init(&bars->k_full[s], 1);
             ptx::mbar_init(&bars->k_empty[s], 1);
-        }
-        for (int s = 0; s < 4; ++s) {
             ptx::mbar_init(&bars->v_full[s], 1);
             ptx::mbar_init(&bars->v_empty[s], 1);
         }
         for (int q = 0; q < 2; ++q) {
+            ptx::mbar_init(&bars->q_full[q], 1);
+            ptx::mbar_init(&bars->q_free[q], 1);
             ptx::mbar_init(&bars->s_full[q], 1);
             ptx::mbar_init(&bars->s_free[q], 8);
             ptx::mbar_init(&bars->p_full[q], 8);
@@ -250,7 +325,12 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             ptx::mbar_init(&bars->o_full[q], 1);
             ptx::mbar_init(&bars->l_full[q], 8);
         }
-        ptx::mbar_init(&bars->l_both, 16);
+        ptx::mbar_init(&bars->o_free, kSmWarps);
+        ptx::mbar_init(&bars->l_both, kSmWarps);
+        for (int s = 0; s < kSlots; ++s) {
+            ptx::mbar_init(&bars->seg_full[s], 1);
+            ptx::mbar_init(&bars->seg_free[s], kRoles);
+        }
         bars->abort_flag = 0;
         ptx::mbar_fence_init();
         ptx::prefetch_tensormap(&tm_q);
@@ -262,21 +342,10 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         ptx::tmem_relinquish();
     }
     ptx::grid_dependency_wait();
-    if (warp == 0) schedule(cache, shape, starts, static_cast<int>(blockIdx.x), &bars->segment, plan);
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = bars->tmem_base;
-    const Segment& seg = bars->segment;
-    const bool whole = seg.whole != 0;
-    const int tiles = seg.b < 0 ? 0 : seg.tile1 - seg.tile0;
-    // The key tiles of a unit: all of them, or every other one.
-    const int steps[2] = {whole ? tiles : (tiles + 1) / 2, whole ? tiles : tiles / 2};
-    const int tile0 = seg.tile0;
-    const int v_stages = L::v_stages(whole);
-    auto k_offset = [](int s) { return L::kKOff + s * L::kTileBytes; };
-    auto v_offset = [](int s) { return s < L::kStages - L::kKStages ? L::kKOff + (L::kKStages + s) * L::kTileBytes : L::kQOff + L::kTileBytes; };
-    auto key_tile = [&](int j, int q) { return tile0 + (whole ? j : 2 * j + q); };
     struct Entry {  // of a ring
         int stage = 0;
         uint32_t phase = 0;
@@ -287,66 +356,138 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
         }
     };
-    int k_loads = 0, v_loads = 0;  // producer: tiles asked for
+    int k_loads = 0, v_loads = 0, q_loads = 0;  // producer: tiles asked for
+    // Every role goes through the same segments.  One whose wait has given up goes on without waiting or computing: the Softmax warps' turns
+    // need each of them, and a segment's place is free when all have been there.
+    Entry slot;
+    bool ok = true;
+    auto segment = [&]() -> const Segment& { return bars->segment[slot.stage]; };
+    auto next_segment = [&]() { return segment_wait(bar_of(offsetof(Barriers, seg_full), slot.stage), slot.phase, abort_flag, kSiteSegment) && segment().b >= 0; };
+    auto done_segment = [&]() {
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&bars->seg_free[slot.stage]);
+        slot.next(kSlots);
+    };
+    // The key tiles of a unit: all of them (whole), or every other one.
+    auto steps_of = [&](const Segment& seg, int q) { return seg.whole ? seg.tile1 - seg.tile0 : (seg.tile1 - seg.tile0 + 1 - q) / 2; };
+    auto key_tile = [&](const Segment& seg, int j, int q) { return seg.tile0 + (seg.whole ? j : 2 * j + q); };
 
-    if (tiles == 0) {
-        // nothing to compute: a segment index behind the last, or a block that sees no key
+    if (warp == kScheduler) {
+        // ================= scheduler: the CTA's segments, one after the other =================
+        Walk walk;
+        const long long cta = blockIdx.x;
+        walk.find(cache, shape, starts, cta);
+        for (;;) {
+            bool more = walk.b >= 0 && walk.begin < (cta + 1) * walk.stretch;
+            Segment s{};
+            s.b = -1;
+            if (more) {
+                const int all = walk.tiles(shape), t0 = walk.tiles_before(shape, cta), t1 = walk.tiles_before(shape, cta + 1);
+                if (t0 < t1 || (all == 0 && walk.begin >= cta * walk.stretch)) {
+                    const int i0 = walk.r * 2 * shape.tile_tokens;
+                    s.b = walk.b;
+                    s.h = walk.h;
+                    s.token0 = min(max(starts[walk.b], 0), shape.tokens) + i0;
+                    s.tokens = walk.share.tokens_of(shape, walk.r);
+                    s.seen0 = walk.share.seen0 + i0;
+                    s.length = walk.share.length;
+                    s.tile0 = t0;
+                    s.tile1 = t1;
+                    s.whole = s.tokens > shape.tile_tokens;
+                    s.q_tile = walk.q_tile0 + 2 * walk.r;
+                    s.part = t1 - t0 == all ? -1 : 2 * static_cast<int>(cta) + (t0 > 0 ? 0 : 1);
+                }
+                walk.next(cache, shape, starts);
+                if (s.b < 0) continue;
+            }
+            if (!segment_wait(bar_of(offsetof(Barriers, seg_free), slot.stage), slot.phase ^ 1u, abort_flag, kSiteSegmentFree)) more = false;
+            if (lane == 0) {
+                bars->segment[slot.stage] = s;
+                ptx::mbar_arrive(&bars->seg_full[slot.stage]);
+            }
+            __syncwarp();
+            slot.next(kSlots);
+            if (!more) break;
+        }
     } else if (warp == kProducer) {
-        // ================= TMA producer: Q once, then the K and V tiles in the order the MMA issuers read them =========
+        // ================= TMA producer: the first keys, Q, then the K and V tiles in the order the MMA issuers read them =========
         // A key tile is up to 8 pages; lane i fetches the part of its page and atom.  Places behind the sequence's length, and pages
         // outside the cache, are fetched from behind the cache: the tensor map fills in zeros.
-        const uint64_t policy = seg.tokens < shape.tile_tokens ? ptx::policy_evict_first() : ptx::policy_evict_last();
-        const int q_rows = shape.tile_tokens * shape.group;
-        if (lane == 0) {
-            ptx::mbar_expect_tx(&bars->q_full, static_cast<uint32_t>((whole ? 2 : 1) * L::kAtoms * q_rows * 128));
-            for (int q = 0; q < (whole ? 2 : 1); ++q)
-                for (int a = 0; a < L::kAtoms; ++a)
-                    ptx::tma_load_4d(smem + L::kQOff + q * L::kTileBytes + a * L::kAtomBytes, &tm_q, &bars->q_full, a * 64, 0, seg.h,
-                                     seg.token0 + q * shape.tile_tokens);
-        }
-        __syncwarp();
+        const uint64_t first_policy = ptx::policy_evict_first(), last_policy = ptx::policy_evict_last();
         const int page_shift = min(cache.page_shift, 7), parts = kTile >> page_shift;  // boxes of a tile, and keys (log2) of a box
         const int part = lane / L::kAtoms, atom = lane % L::kAtoms;
         const bool fetches = part < parts;
-        const int* table = cache.table + static_cast<size_t>(seg.b) * cache.table_width;
-        auto place = [&](int kt) {  // the page's place among those of all heads
-            const int at = kt * kTile + (part << page_shift);
-            int p = -1;
-            if (fetches && at < seg.length) p = table[at >> cache.page_shift];
-            return static_cast<unsigned>(p) < static_cast<unsigned>(cache.pages) ? p * cache.kv_heads + seg.h : cache.pages * cache.kv_heads;
-        };
-        Entry ek, ev;
-        bool ok = true;
-        auto load = [&](const CUtensorMap* map, uint32_t full, uint32_t empty, uint32_t phase, uint8_t* dst, int kt, int where) {
-            if (!ok) return;
-            ok = warp_wait(empty, phase ^ 1u, abort_flag, kSiteProducerEmpty);
-            if (!ok) return;
-            if (lane == 0) ptx::mbar_expect_tx(full, static_cast<uint32_t>(L::kTileBytes));
-            __syncwarp();
-            if (fetches)
-                ptx::tma_load_3d(dst + atom * L::kAtomBytes + (part << page_shift) * 128, map, full, atom * 64,
-                                 (kt * kTile) & ((1 << cache.page_shift) - 1) & ~(kTile - 1), where, policy);
-            __syncwarp();
-        };
-        auto load_k = [&](int kt, int where) {
-            load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), bar_of(offsetof(Barriers, k_empty), ek.stage), ek.phase, smem + k_offset(ek.stage), kt, where);
-            ek.next(L::kKStages);
-            k_loads += ok ? 1 : 0;
-        };
-        auto load_v = [&](int kt, int where) {
-            load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), bar_of(offsetof(Barriers, v_empty), ev.stage), ev.phase, smem + v_offset(ev.stage), kt, where);
-            ev.next(v_stages);
-            v_loads += ok ? 1 : 0;
-        };
-        const int lists = whole ? 1 : 2;  // units that have key tiles of their own
-        int where_k[2] = {place(key_tile(0, 0)), lists > 1 && steps[1] > 0 ? place(key_tile(0, 1)) : 0}, where_v[2] = {0, 0};
-        for (int j = -1; ok && j < steps[0]; ++j) {
-            for (int q = 0; q < lists; ++q) {
-                const int next = where_k[q];
-                if (j + 2 < steps[q]) where_k[q] = place(key_tile(j + 2, q));  // a step ahead of its use
-                if (j + 1 < steps[q]) load_k(key_tile(j + 1, q), next);
-                if (j >= 0 && j < steps[q]) load_v(key_tile(j, q), where_v[q]);
-                where_v[q] = next;
+        const uint32_t q_bytes = static_cast<uint32_t>(L::kAtoms * shape.tile_tokens * shape.group * 128);
+        Entry ek, ev, eq;
+        for (; next_segment(); done_segment()) {
+            const Segment& seg = segment();
+            const int tiles = seg.tile1 - seg.tile0, tile0 = seg.tile0, length = seg.length, h = seg.h;
+            const uint64_t policy = seg.tokens < shape.tile_tokens ? first_policy : last_policy;
+            const int* table = cache.table + static_cast<size_t>(seg.b) * cache.table_width;
+            if (!ok || tiles == 0) continue;
+            auto place = [&](int kt) {  // the page's place among those of all heads
+                const int at = kt * kTile + (part << page_shift);
+                int p = -1;
+                if (fetches && kt < seg.tile1 && at < length) p = table[at >> cache.page_shift];
+                return static_cast<unsigned>(p) < static_cast<unsigned>(cache.pages) ? p * cache.kv_heads + h : cache.pages * cache.kv_heads;
+            };
+            auto load = [&](const CUtensorMap* map, uint32_t full, uint8_t* dst, int kt, int where) {
+                if (lane == 0) ptx::mbar_expect_tx(full, static_cast<uint32_t>(L::kTileBytes));
+                __syncwarp();
+                if (fetches)
+                    ptx::tma_load_3d(dst + atom * L::kAtomBytes + (part << page_shift) * 128, map, full, atom * 64,
+                                     (kt * kTile) & ((1 << cache.page_shift) - 1) & ~(kTile - 1), where, policy);
+                __syncwarp();
+            };
+            auto load_q = [&](int q) {
+                ok = ok && warp_wait(bar_of(offsetof(Barriers, q_free), eq.stage), eq.phase ^ 1u, abort_flag, kSiteQFree);
+                if (!ok) return;
+                if (lane == 0) {
+                    ptx::mbar_expect_tx(&bars->q_full[eq.stage], q_bytes);
+                    for (int a = 0; a < L::kAtoms; ++a)
+                        ptx::tma_load_4d(smem + L::kQOff + eq.stage * L::kTileBytes + a * L::kAtomBytes, &tm_q, &bars->q_full[eq.stage], a * 64, 0, h,
+                                         seg.token0 + q * shape.tile_tokens);
+                }
+                __syncwarp();
+                eq.next(2);
+                ++q_loads;
+            };
+            // Both kinds in the order of the keys (split: the units take them in turn), each as soon as it has room.
+            int k = 0, v = 0, where_k = place(tile0), where_v = where_k;
+            long long idle_since = 0;
+            while (ok && v < tiles) {
+                bool idle = true;
+                if (k < tiles && __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(offsetof(Barriers, k_empty), ek.stage), ek.phase ^ 1u))) {
+                    load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), smem + L::kKOff + ek.stage * L::kTileBytes, tile0 + k, where_k);
+                    ek.next(L::kStages);
+                    ++k_loads;
+                    if (k == 0) {
+                        load_q(0);
+                        if (seg.whole) load_q(1);
+                    }
+                    where_k = place(tile0 + ++k);
+                    idle = false;
+                }
+                if (ok && v < k && __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(offsetof(Barriers, v_empty), ev.stage), ev.phase ^ 1u))) {
+                    load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), smem + L::kVOff + ev.stage * L::kTileBytes, tile0 + v, where_v);
+                    ev.next(L::kStages);
+                    ++v_loads;
+                    where_v = place(tile0 + ++v);
+                    idle = false;
+                }
+                if (!idle) {
+                    idle_since = 0;
+                    continue;
+                }
+                const long long now = clock64();
+                if (idle_since == 0) idle_since = now;
+                bool give_up = *abort_flag != 0u;
+                if (!give_up && now - idle_since > kWaitLimitCycles) {
+                    *abort_flag = 1;
+                    atomicCAS(&g_attnw_status, 0u, 0x80000000u | kSiteProducerEmpty);
+                    give_up = true;
+                }
+                ok = !__any_sync(0xffffffffu, give_up);
             }
         }
     } else if (warp == kMma || warp == kMmaProduct) {
@@ -355,90 +496,120 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         constexpr uint32_t idesc_o = ptx::umma_idesc_bf16_f32(kTile, D) | (1u << 16);  // B operand MN-major
         const uint32_t base = ptx::smem_u32(smem);
         // Did an earlier launch give up?  Then this one computes and writes nothing.
-        const uint32_t prior_failure = *reinterpret_cast<volatile unsigned int*>(&g_attnw_status);
-        bool ok = warp_wait(bar_of(offsetof(Barriers, q_full), 0), 0, abort_flag, kSiteMmaQ);
-        if (__any_sync(0xffffffffu, prior_failure != 0u)) {
+        if (__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u)) {
             *abort_flag = 1;
             ok = false;
         }
         Entry e;  // of the issuer's own ring
         auto arrived = [&](size_t full) { ok = ok && warp_wait(bar_of(full, e.stage), e.phase, abort_flag, kSiteMmaKFull); };
-        auto release = [&](uint64_t* empty, int stages) {  // the tile may be replaced once the MMAs issued so far are complete
-            if (ptx::elect_one()) ptx::umma_commit(empty + e.stage);
+        auto release = [&](uint64_t* empty) {  // the tile may be replaced once the MMAs issued so far are complete
+            if (ok && ptx::elect_one()) ptx::umma_commit(empty + e.stage);
             __syncwarp();
-            e.next(stages);
+            e.next(L::kStages);
         };
-        int last_q = 0, last_j = -1;  // kSharedS: whose scores the buffer holds
-        auto scores = [&](int q, int j) {  // S of step j
-            const int before_q = L::kSharedS ? last_q : q, before_j = L::kSharedS ? last_j : j - 1;
-            ok = ok && warp_wait(bar_of(offsetof(Barriers, s_free), before_q), static_cast<uint32_t>(before_j) & 1u, abort_flag, kSiteMmaSFree);
-            if (!ok) return;
-            last_q = q;
-            last_j = j;
-            ptx::tc_fence_after_sync();
-            const uint32_t d_tmem = tmem_base + L::s_col(q);
-            const uint64_t a_desc = ptx::umma_desc_kmajor_sw128(base + L::kQOff + (whole ? static_cast<uint32_t>(q * L::kTileBytes) : 0u));
-            const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(k_offset(e.stage)));
-            if (ptx::elect_one()) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint64_t off = static_cast<uint64_t>(((k >> 2) * L::kAtomBytes + (k & 3) * 32) >> 4);
-                    ptx::umma_f16_ss(d_tmem, a_desc + off, b_desc + off, idesc_s, k > 0 ? 1u : 0u);
-                }
-                ptx::umma_commit(&bars->s_full[q]);
-            }
-            __syncwarp();
-        };
-        auto product = [&](int q, int j) {  // O += P V of step j
-            ok = ok && warp_wait(bar_of(offsetof(Barriers, p_full), q), static_cast<uint32_t>(j) & 1u, abort_flag, kSiteMmaPFull);
-            if (!ok) return;
-            ptx::tc_fence_after_sync();
-            const uint32_t o_tmem = tmem_base + L::o_col(q), p_tmem = tmem_base + L::p_col(q);
-            const uint64_t b_desc = av::umma_desc_mnmajor_sw128(base + static_cast<uint32_t>(v_offset(e.stage)), L::kAtomBytes);
-            if (ptx::elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per instruction
-                    ptx::umma_f16_ts(o_tmem, p_tmem + static_cast<uint32_t>(kk * 8), b_desc + static_cast<uint64_t>(kk * 16 * 128 >> 4), idesc_o,
-                                     (j > 0 || kk > 0) ? 1u : 0u);
-                ptx::umma_commit(&bars->p_free[q]);
-                if (j + 1 == steps[q]) ptx::umma_commit(&bars->o_full[q]);
-            }
-            __syncwarp();
-        };
-        // The values behind the sequence's length may be anything, NaN too, and a weight of zero does not silence that: such rows become zeros.
-        auto clear_unused = [&](int kt) {
-            const int used = seg.length - kt * kTile;
-            if (!ok || used >= kTile) return;
-            uint8_t* rows = smem + v_offset(e.stage);
-            for (int i = max(used, 0) * 8 + lane; i < kTile * 8; i += 32)
-                for (int a = 0; a < L::kAtoms; ++a) *reinterpret_cast<uint4*>(rows + a * L::kAtomBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-        };
+        uint32_t done[2] = {0, 0};  // steps of each unit so far
         if (warp == kMma) {
-            for (int j = 0; ok && j < steps[0]; ++j) {
-                for (int q = 0; ok && q < (whole ? 1 : 2); ++q) {
-                    if (j >= steps[q]) continue;
-                    arrived(offsetof(Barriers, k_full));
-                    scores(q, j);
-                    if (whole) scores(1, j);
-                    release(bars->k_empty, L::kKStages);
+            Entry eq;
+            int last = 0;          // kSharedS: the unit whose scores the buffer holds, and the number of its step
+            uint32_t last_step = 0xffffffffu;
+            auto scores = [&](int q, uint32_t step, int q_place) {
+                const int before = L::kSharedS ? last : q;
+                const uint32_t before_step = L::kSharedS ? last_step : step - 1u;
+                ok = ok && warp_wait(bar_of(offsetof(Barriers, s_free), before), before_step & 1u, abort_flag, kSiteMmaSFree);
+                if (!ok) return;
+                last = q;
+                last_step = step;
+                ptx::tc_fence_after_sync();
+                const uint32_t d_tmem = tmem_base + L::s_col(q);
+                const uint64_t a_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(L::kQOff + q_place * L::kTileBytes));
+                const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(L::kKOff + e.stage * L::kTileBytes));
+                if (ptx::elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint64_t off = static_cast<uint64_t>(((k >> 2) * L::kAtomBytes + (k & 3) * 32) >> 4);
+                        ptx::umma_f16_ss(d_tmem, a_desc + off, b_desc + off, idesc_s, k > 0 ? 1u : 0u);
+                    }
+                    ptx::umma_commit(&bars->s_full[q]);
                 }
+                __syncwarp();
+            };
+            for (; next_segment(); done_segment()) {
+                const Segment& seg = segment();
+                const bool whole = seg.whole != 0;
+                const int steps[2] = {steps_of(seg, 0), steps_of(seg, 1)};
+                if (!ok || steps[0] == 0) continue;
+                const int place0 = eq.stage, place1 = whole ? place0 ^ 1 : place0;
+                for (int q = 0; q < (whole ? 2 : 1); ++q) {
+                    ok = ok && warp_wait(bar_of(offsetof(Barriers, q_full), eq.stage), eq.phase, abort_flag, kSiteMmaQ);
+                    eq.next(2);
+                }
+                for (int j = 0; ok && j < steps[0]; ++j) {
+                    for (int q = 0; ok && q < (whole ? 1 : 2); ++q) {
+                        if (j >= steps[q]) continue;
+                        arrived(offsetof(Barriers, k_full));
+                        scores(q, done[q] + static_cast<uint32_t>(j), q == 0 ? place0 : place1);
+                        if (whole) scores(1, done[1] + static_cast<uint32_t>(j), place1);
+                        release(bars->k_empty);
+                    }
+                }
+                if (ok && ptx::elect_one()) {
+                    ptx::umma_commit(&bars->q_free[place0]);
+                    if (whole) ptx::umma_commit(&bars->q_free[place1]);
+                }
+                __syncwarp();
+                done[0] += static_cast<uint32_t>(steps[0]);
+                done[1] += static_cast<uint32_t>(steps[1]);
             }
         } else {
-            for (int j = 0; ok && j < steps[0]; ++j) {
-                for (int q = 0; ok && q < (whole ? 1 : 2); ++q) {
-                    if (j >= steps[q]) continue;
-                    arrived(offsetof(Barriers, v_full));
-                    clear_unused(key_tile(j, q));
-                    product(q, j);
-                    if (whole) product(1, j);
-                    release(bars->v_empty, v_stages);
+            uint32_t splits = 0;  // segments so far whose O both units read
+            auto product = [&](const Segment& seg, int q, int j, int steps) {  // O += P V of step j
+                ok = ok && warp_wait(bar_of(offsetof(Barriers, p_full), q), (done[q] + static_cast<uint32_t>(j)) & 1u, abort_flag, kSiteMmaPFull);
+                if (!ok) return;
+                ptx::tc_fence_after_sync();
+                const uint32_t o_tmem = tmem_base + L::o_col(q), p_tmem = tmem_base + L::p_col(q);
+                const uint64_t b_desc = av::umma_desc_mnmajor_sw128(base + static_cast<uint32_t>(L::kVOff + e.stage * L::kTileBytes), L::kAtomBytes);
+                if (ptx::elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per instruction
+                        ptx::umma_f16_ts(o_tmem, p_tmem + static_cast<uint32_t>(kk * 8), b_desc + static_cast<uint64_t>(kk * 16 * 128 >> 4), idesc_o,
+                                         (j > 0 || kk > 0) ? 1u : 0u);
+                    ptx::umma_commit(&bars->p_free[q]);
+                    if (j + 1 == steps) ptx::umma_commit(&bars->o_full[q]);
                 }
+                __syncwarp();
+            };
+            // The values behind the sequence's length may be anything, NaN too, and a weight of zero does not silence that: such rows become zeros.
+            auto clear_unused = [&](int used) {
+                if (!ok || used >= kTile) return;
+                uint8_t* rows = smem + L::kVOff + e.stage * L::kTileBytes;
+                for (int i = max(used, 0) * 8 + lane; i < kTile * 8; i += 32)
+                    for (int a = 0; a < L::kAtoms; ++a) *reinterpret_cast<uint4*>(rows + a * L::kAtomBytes + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+            };
+            for (; next_segment(); done_segment()) {
+                const Segment& seg = segment();
+                const bool whole = seg.whole != 0;
+                const int steps[2] = {steps_of(seg, 0), steps_of(seg, 1)};
+                if (!ok || steps[0] == 0) continue;
+                // (a unit's own warps have read its O when its P arrives; the other unit's, of a split segment, too?)
+                if (splits > 0) ok = warp_wait(bar_of(offsetof(Barriers, o_free), 0), (splits - 1u) & 1u, abort_flag, kSiteOFree);
+                for (int j = 0; ok && j < steps[0]; ++j) {
+                    for (int q = 0; ok && q < (whole ? 1 : 2); ++q) {
+                        if (j >= steps[q]) continue;
+                        arrived(offsetof(Barriers, v_full));
+                        clear_unused(seg.length - key_tile(seg, j, q) * kTile);
+                        product(seg, q, j, steps[q]);
+                        if (whole) product(seg, 1, j, steps[1]);
+                        release(bars->v_empty);
+                    }
+                }
+                if (!whole) ++splits;
+                done[0] += static_cast<uint32_t>(steps[0]);
+                done[1] += static_cast<uint32_t>(steps[1]);
             }
         }
-    }
-    if (warp < kSmWarps && seg.b >= 0) {
+    } else {
         // ================= Softmax warps: two threads per query row, 64 key columns of a tile each =================
         const int q = warp >> 3;
         const int half = (warp >> 2) & 1;
@@ -449,223 +620,240 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const float c2 = scale_log2e;
         const uint64_t c2c2 = ptx::pack2(c2, c2);
         const int row = quarter * 32 + lane;
-        float* const stats = reinterpret_cast<float*>(smem + L::kStatOff) + q * kUnitStats;
-        const uint32_t max_own = ptx::smem_u32(stats + half * kTile + row), max_other = ptx::smem_u32(stats + (half ^ 1) * kTile + row);
+        const int in_tile = row / shape.group;  // the row's token in its query tile
+        const uint32_t max_own = ptx::smem_u32(smem + L::kStatOff) + static_cast<uint32_t>((q * 4 * kTile + half * kTile + row) * 4);
+        const uint32_t max_other = ptx::smem_u32(smem + L::kStatOff) + static_cast<uint32_t>((q * 4 * kTile + (half ^ 1) * kTile + row) * 4);
         const uint32_t lane0 = lane == 0;
         const uint32_t p_own = t_quarter + L::p_col(q) + static_cast<uint32_t>(half * 32);  // its 64 keys of P
-        // The row's token (of the block), and the keys that it sees: a token more for each row of G.  A row that is none's gets what its place would.
-        const int tile_first = whole ? q * shape.tile_tokens : 0;  // the first token of this unit's query tile
-        const int token = tile_first + row / shape.group;
-        const int seen = min(max(seg.seen0 + token, 0), seg.length);
-        const int seen_least = min(max(seg.seen0 + tile_first, 0), seg.length);  // of the tile's rows
-        float smax = -3.0e38f;  // running maximum of the raw scores of this row (all columns)
-        float mb = -3.0e38f;    // the offset the weights, l and O's row are relative to (follows smax * c2 lazily)
-        float l = 0.0f;         // sum of this thread's weights
-        bool ok = true;
-        const int my_steps = q == 0 ? steps[0] : steps[1], other_steps = q == 0 ? steps[1] : steps[0];
         // The units take turns at the exponentials (see attn_onepass.cuh); the barrier of a turn is the one that the two threads of a row exchange
         // their maxima by.  Every warp takes part in all of them, also after a wait has given up.
         const uint32_t turn_own = static_cast<uint32_t>(1 + q * 4 + quarter), turn_other = static_cast<uint32_t>(1 + (q ^ 1) * 4 + quarter);
         const int behind = q == 0 ? 1 : 0;
-        auto take_turn = [&](int j) { ptx::named_sync(turn_own, j >= behind && j - behind < other_steps ? 128u : 64u); };
-        auto pass_turn = [&](int j) {
-            if (j + 1 - behind < other_steps) ptx::named_arrive(turn_other, 128u);
-        };
-        for (int j = 0; j < my_steps; ++j) {
-            if (ok) ok = warp_wait(bar_of(offsetof(Barriers, s_full), q), static_cast<uint32_t>(j) & 1u, abort_flag, kSiteSFull);
-            if (!ok) {
-                take_turn(j);
-                pass_turn(j);
-                continue;
-            }
-            ptx::tc_fence_after_sync();
-            const int tile_begin = key_tile(j, q) * kTile;
-            const bool masked = seen_least - tile_begin < kTile;  // for some row of the tile
-            const int valid = seen - tile_begin - half * kHalf;   // of this thread's columns
-            float s[kHalf];
-            {
-                uint32_t r0[kChunk], r1[kChunk];
-                ptx::tmem_ld_32x32b_x32(t_own, r0);
-                ptx::tmem_ld_32x32b_x32(t_own + kChunk, r1);
-                ptx::tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) {
-                    s[i] = __uint_as_float(r0[i]);
-                    s[kChunk + i] = __uint_as_float(r1[i]);
+        uint32_t phases = 0;  // bit 0: parity of the unit's steps so far; 1, 2: of its segments with a step, of the other unit's; 3, 4: of whole and split segments
+        for (; next_segment(); done_segment()) {
+            const Segment& seg = segment();
+            const bool whole = seg.whole != 0;
+            const int my_steps = steps_of(seg, q), other_steps = steps_of(seg, q ^ 1);
+            const int tiles = seg.tile1 - seg.tile0;
+            // The row's token (of the block), and the keys that it sees.  A row that is none's gets what its place would.
+            const int tile_first = whole ? q * shape.tile_tokens : 0;  // the first token of this unit's query tile
+            const int seen = min(max(seg.seen0 + tile_first + in_tile, 0), seg.length);
+            const int seen_least = min(max(seg.seen0 + tile_first, 0), seg.length);  // of the tile's rows
+            float smax = -3.0e38f;  // running maximum of the raw scores of this row (all columns)
+            float mb = -3.0e38f;    // the offset the weights, l and O's row are relative to (follows smax * c2 lazily)
+            float l = 0.0f;         // sum of this thread's weights
+            auto take_turn = [&](int j) { ptx::named_sync(turn_own, j >= behind && j - behind < other_steps ? 128u : 64u); };
+            auto pass_turn = [&](int j) {
+                if (j + 1 - behind < other_steps) ptx::named_arrive(turn_other, 128u);
+            };
+            const int tile_step = whole ? kTile : 2 * kTile;
+            int tile_begin = key_tile(seg, 0, q) * kTile;
+            for (int j = 0; j < my_steps; ++j, tile_begin += tile_step) {
+                const uint32_t parity = (phases + static_cast<uint32_t>(j)) & 1u;
+                if (ok) ok = warp_wait(bar_of(offsetof(Barriers, s_full), q), parity, abort_flag, kSiteSFull);
+                if (!ok) {
+                    take_turn(j);
+                    pass_turn(j);
+                    continue;
                 }
-            }
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&bars->s_free[q]);
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < kHalf; ++i)
-                    if (i >= valid) s[i] = -3.0e38f;
-            }
-            // ---- row maximum, lazy offset ----
-            float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
-#pragma unroll
-            for (int i = 4; i < kHalf; i += 8) {
-                m0 = ptx::max3(m0, s[i + 0], s[i + 1]);
-                m1 = ptx::max3(m1, s[i + 2], s[i + 3]);
-                if (i + 4 < kHalf) {
-                    m2 = ptx::max3(m2, s[i + 4], s[i + 5]);
-                    m3 = ptx::max3(m3, s[i + 6], s[i + 7]);
-                }
-            }
-            m0 = ptx::max3(fmaxf(m0, m1), m2, m3);
-            const uint32_t slot = static_cast<uint32_t>(j & 1) * (2 * kTile * 4);
-            ptx::st_shared_f32(max_own + slot, m0);
-            ok = static_cast<bool>(
-                __all_sync(0xffffffffu, av1::wait_in_place(&bars->p_free[q], (static_cast<uint32_t>(j) & 1u) ^ 1u, abort_flag, kSitePFree)));
-            take_turn(j);
-            if (!ok) {
-                pass_turn(j);
-                continue;
-            }
-            smax = ptx::max3(smax, m0, ptx::ld_shared_f32(max_other + slot));
-            const float mb_cand = fmaxf(smax * c2, -3.0e38f);
-            const bool move = j == 0 || mb_cand - mb > kLazy;
-            ptx::tc_fence_after_sync();
-            uint32_t w[16];  // 32 keys of P on their way to tensor memory
-            if (j == 0) {
-                mb = mb_cand;
-            } else if (__any_sync(0xffffffffu, move)) {
-                const float alpha = move ? ptx::ex2_approx(mb - mb_cand) : 1.0f;
-                if (move) mb = mb_cand;
-                l *= alpha;
                 ptx::tc_fence_after_sync();
-#pragma unroll 1
-                for (int c = 0; c < D / 2; c += 8) {  // 8 columns at a time: the row of scores stays in registers
-                    uint32_t r[8];
-                    ptx::tmem_ld_32x32b_x8(o_own + static_cast<uint32_t>(c), r);
+                const bool masked = seen_least - tile_begin < kTile;  // for some row of the tile
+                const int valid = seen - tile_begin - half * kHalf;   // of this thread's columns
+                float s[kHalf];
+                {
+                    uint32_t r0[kChunk], r1[kChunk];
+                    ptx::tmem_ld_32x32b_x32(t_own, r0);
+                    ptx::tmem_ld_32x32b_x32(t_own + kChunk, r1);
                     ptx::tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                    ptx::tmem_st_32x32b_x8(o_own + static_cast<uint32_t>(c), r);
-                }
-                ptx::tmem_wait_st();
-            }
-            // ---- weights: p = 2^(c2 s - mb) (below 2^8), row sum, bf16, into tensor memory ----
-            const uint64_t nmb2 = ptx::pack2(-mb, -mb);
-            uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll
-            for (int g = 0; g < kHalf / 8; ++g) {
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    float x0, x1;
-                    ptx::unpack2(ptx::fma2(ptx::pack2(s[g * 8 + i], s[g * 8 + i + 1]), c2c2, nmb2), x0, x1);
-                    p[i] = ptx::ex2_approx(x0);
-                    p[i + 1] = ptx::ex2_approx(x1);
-                    if (masked) {  // weight zero
-                        p[i] = (g * 8 + i < valid) ? p[i] : 0.0f;
-                        p[i + 1] = (g * 8 + i + 1 < valid) ? p[i + 1] : 0.0f;
+                    for (int i = 0; i < kChunk; ++i) {
+                        s[i] = __uint_as_float(r0[i]);
+                        s[kChunk + i] = __uint_as_float(r1[i]);
                     }
-                    acc[(i >> 1) & 3] = ptx::add2(acc[(i >> 1) & 3], ptx::pack2(p[i], p[i + 1]));
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[(g & 3) * 4 + i] = ptx::pack_bf16x2(p[2 * i], p[2 * i + 1]);
-                if (g == kPassAt) pass_turn(j);
-                if ((g & 3) == 3) ptx::tmem_st_32x32b_x16(p_own + static_cast<uint32_t>((g >> 2) * 16), w);
-            }
-            float a0, a1, a2, a3;
-            ptx::unpack2(ptx::add2(acc[0], acc[1]), a0, a1);
-            ptx::unpack2(ptx::add2(acc[2], acc[3]), a2, a3);
-            l += (a0 + a1) + (a2 + a3);
-            ptx::tmem_wait_st();
-            ptx::tc_fence_before_sync();  // orders P in tensor memory and the rescale of O before the MMAs that use them
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&bars->p_full[q]);
-        }
-
-        // ---- epilogue ----
-        // The rows' statistics meet in shared memory: whole, those of the two threads of a row; split, of its four, who take D / 4 columns each of
-        // 2^(mb_0 - mb) O_0 + 2^(mb_1 - mb) O_1.
-        if (tiles > 0) {
-            if (ok && my_steps > 0) ok = warp_wait(bar_of(offsetof(Barriers, o_full), q), 0, abort_flag, kSiteOFull);
-            if (ok && !whole && other_steps > 0) ok = warp_wait(bar_of(offsetof(Barriers, o_full), q ^ 1), 0, abort_flag, kSiteOFull);
-            if (ok) {
-                stats[half * kTile + row] = l;  // (the maxima have all been read: the last product has them behind it)
-                if (half == 0) stats[2 * kTile + row] = mb;
+                ptx::tc_fence_before_sync();
                 __syncwarp();
-                const uint32_t l_bar = whole ? bar_of(offsetof(Barriers, l_full), q) : bar_of(offsetof(Barriers, l_both), 0);
-                ptx::mbar_arrive_if(l_bar, lane0);
-                ok = warp_wait(l_bar, 0, abort_flag, kSiteLFull);
-            }
-        } else {
-            ok = *reinterpret_cast<volatile unsigned int*>(&g_attnw_status) == 0u;
-        }
-        if (ok) {
-            float l_row = 0.0f, top = -3.0e38f, f_own = 0.0f, f_other = 0.0f;
-            if (tiles > 0) {
-                const float* peer = reinterpret_cast<const float*>(smem + L::kStatOff) + (q ^ 1) * kUnitStats;
-                const float l_own = l + stats[(half ^ 1) * kTile + row];
-                l_row = l_own;
-                top = mb;
-                f_own = 1.0f;
-                if (!whole) {
-                    const float l_other = peer[row] + peer[kTile + row], mb_other = peer[2 * kTile + row];
-                    // (a unit that has seen nothing of the row has a sum of zero, and its offset no say)
-                    top = l_own > 0.0f ? (l_other > 0.0f ? fmaxf(mb, mb_other) : mb) : mb_other;
-                    f_own = l_own > 0.0f ? ptx::ex2_approx(mb - top) : 0.0f;
-                    f_other = l_other > 0.0f ? ptx::ex2_approx(mb_other - top) : 0.0f;
-                    l_row = l_own * f_own + l_other * f_other;
+                if (lane == 0) ptx::mbar_arrive(&bars->s_free[q]);
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < kHalf; ++i)
+                        if (i >= valid) s[i] = -3.0e38f;
                 }
-            }
-            const bool joined = seg.segments > 1;  // by combine_kernel
-            if (!joined) {
-                const float inv = l_row > 0.0f ? 1.0f / l_row : 0.0f;
-                f_own *= inv;
-                f_other *= inv;
-            }
-            ptx::tc_fence_after_sync();
-            const int in_tile = row / shape.group, g = row - in_tile * shape.group;
-            const bool stored = in_tile < shape.tile_tokens && token < seg.tokens && (whole || tiles > 0 || q == 0);
-            const int cols = whole || tiles == 0 ? D / 2 : D / 4;
-            const int col0 = whole || tiles == 0 ? half * (D / 2) : (q * 2 + half) * (D / 4);
-            const size_t out_row = static_cast<size_t>(seg.token0 + token) * shape.heads + seg.h * shape.group + g;
-            const size_t part_row = static_cast<size_t>(seg.part) + token * shape.group + g;
-            if (stored && half == 0 && (whole || q == 0)) {
-                if (joined)
-                    part_stats[part_row] = make_float2(top, l_row);
-                else
-                    store_lse(cache, shape, lse, lse2, out_row, seg.q_tile + (whole ? q : 0), seg.h, row, top, l_row);
-            }
-            __syncwarp();
-            const uint32_t o_unit = t_quarter + L::o_col(q), o_peer = t_quarter + L::o_col(q ^ 1);
-            const bool has_own = tiles > 0 && my_steps > 0, has_other = tiles > 0 && !whole && other_steps > 0;
+                // ---- row maximum, lazy offset ----
+                float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
+#pragma unroll
+                for (int i = 4; i < kHalf; i += 8) {
+                    m0 = ptx::max3(m0, s[i + 0], s[i + 1]);
+                    m1 = ptx::max3(m1, s[i + 2], s[i + 3]);
+                    if (i + 4 < kHalf) {
+                        m2 = ptx::max3(m2, s[i + 4], s[i + 5]);
+                        m3 = ptx::max3(m3, s[i + 6], s[i + 7]);
+                    }
+                }
+                m0 = ptx::max3(fmaxf(m0, m1), m2, m3);
+                const uint32_t place = parity * (2 * kTile * 4);
+                ptx::st_shared_f32(max_own + place, m0);
+                ok = static_cast<bool>(__all_sync(0xffffffffu, av1::wait_in_place(&bars->p_free[q], parity ^ 1u, abort_flag, kSitePFree)));
+                take_turn(j);
+                if (!ok) {
+                    pass_turn(j);
+                    continue;
+                }
+                smax = ptx::max3(smax, m0, ptx::ld_shared_f32(max_other + place));
+                const float mb_cand = fmaxf(smax * c2, -3.0e38f);
+                const bool move = j == 0 || mb_cand - mb > kLazy;
+                ptx::tc_fence_after_sync();
+                uint32_t w[16];  // 32 keys of P on their way to tensor memory
+                if (j == 0) {
+                    mb = mb_cand;
+                } else if (__any_sync(0xffffffffu, move)) {
+                    const float alpha = move ? ptx::ex2_approx(mb - mb_cand) : 1.0f;
+                    if (move) mb = mb_cand;
+                    l *= alpha;
+                    ptx::tc_fence_after_sync();
 #pragma unroll 1
-            for (int c = col0; c < col0 + cols; c += 16) {
-                float v[16];
-                uint32_t o[16];
+                    for (int c = 0; c < D / 2; c += 8) {  // 8 columns at a time: the row of scores stays in registers
+                        uint32_t r[8];
+                        ptx::tmem_ld_32x32b_x8(o_own + static_cast<uint32_t>(c), r);
+                        ptx::tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                if (has_own) {
-                    ptx::tmem_ld_32x32b_x16(o_unit + static_cast<uint32_t>(c), o);
-                    ptx::tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(o[i]) * f_own;
+                        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                        ptx::tmem_st_32x32b_x8(o_own + static_cast<uint32_t>(c), r);
+                    }
+                    ptx::tmem_wait_st();
                 }
-                if (has_other) {
-                    ptx::tmem_ld_32x32b_x16(o_peer + static_cast<uint32_t>(c), o);
-                    ptx::tmem_wait_ld();
+                // ---- weights: p = 2^(c2 s - mb) (below 2^8), row sum, bf16, into tensor memory ----
+                const uint64_t nmb2 = ptx::pack2(-mb, -mb);
+                uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = fmaf(__uint_as_float(o[i]), f_other, v[i]);
+                for (int g = 0; g < kHalf / 8; ++g) {
+                    float p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        float x0, x1;
+                        ptx::unpack2(ptx::fma2(ptx::pack2(s[g * 8 + i], s[g * 8 + i + 1]), c2c2, nmb2), x0, x1);
+                        p[i] = ptx::ex2_approx(x0);
+                        p[i + 1] = ptx::ex2_approx(x1);
+                        if (masked) {  // weight zero
+                            p[i] = (g * 8 + i < valid) ? p[i] : 0.0f;
+                            p[i + 1] = (g * 8 + i + 1 < valid) ? p[i + 1] : 0.0f;
+                        }
+                        acc[(i >> 1) & 3] = ptx::add2(acc[(i >> 1) & 3], ptx::pack2(p[i], p[i + 1]));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[(g & 3) * 4 + i] = ptx::pack_bf16x2(p[2 * i], p[2 * i + 1]);
+                    if (g == kPassAt) pass_turn(j);
+                    if ((g & 3) == 3) ptx::tmem_st_32x32b_x16(p_own + static_cast<uint32_t>((g >> 2) * 16), w);
                 }
-                // (no branch around the rest of the loop: the loads of the next columns are the whole warp's)
-                if (stored && joined) {
-                    float4* dst = reinterpret_cast<float4*>(part_o + part_row * D + c);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                } else if (stored) {
-                    uint4* dst = reinterpret_cast<uint4*>(O + out_row * D + c);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        dst[i] = make_uint4(ptx::pack_bf16x2(v[8 * i], v[8 * i + 1]), ptx::pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                                            ptx::pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), ptx::pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+                float a0, a1, a2, a3;
+                ptx::unpack2(ptx::add2(acc[0], acc[1]), a0, a1);
+                ptx::unpack2(ptx::add2(acc[2], acc[3]), a2, a3);
+                l += (a0 + a1) + (a2 + a3);
+                ptx::tmem_wait_st();
+                ptx::tc_fence_before_sync();  // orders P in tensor memory and the rescale of O before the MMAs that use them
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&bars->p_full[q]);
+            }
+
+            // ---- the segment's result ----
+            // The rows' statistics meet in shared memory: whole, those of the two threads of a row; split, of its four, who take D / 4 columns each of
+            // 2^(mb_0 - mb) O_0 + 2^(mb_1 - mb) O_1.
+            float* const sums = reinterpret_cast<float*>(smem + L::kSumOff) + q * 3 * kTile + row;
+            const float* const peer = reinterpret_cast<const float*>(smem + L::kSumOff) + (q ^ 1) * 3 * kTile + row;
+            if (tiles > 0) {
+                if (ok && my_steps > 0) ok = warp_wait(bar_of(offsetof(Barriers, o_full), q), (phases >> 1) & 1u, abort_flag, kSiteOFull);
+                if (ok && !whole && other_steps > 0) ok = warp_wait(bar_of(offsetof(Barriers, o_full), q ^ 1), (phases >> 2) & 1u, abort_flag, kSiteOFull);
+                if (ok) {
+                    // (nobody reads the last segment's any more: this one's products came behind that)
+                    if (my_steps > 0) {
+                        sums[half * kTile] = l;
+                        if (half == 0) sums[2 * kTile] = mb;
+                    }
+                    __syncwarp();
+                    const uint32_t l_bar = whole ? bar_of(offsetof(Barriers, l_full), q) : bar_of(offsetof(Barriers, l_both), 0);
+                    ptx::mbar_arrive_if(l_bar, lane0);
+                    ok = warp_wait(l_bar, (phases >> (whole ? 3 : 4)) & 1u, abort_flag, kSiteLFull);
+                }
+            } else if (ok) {
+                ok = !__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u);
+            }
+            if (ok) {
+                float l_row = 0.0f, top = -3.0e38f, f_own = 0.0f, f_other = 0.0f;
+                if (tiles > 0) {
+                    const float l_own = my_steps > 0 ? l + sums[(half ^ 1) * kTile] : 0.0f;
+                    l_row = l_own;
+                    top = mb;
+                    f_own = 1.0f;
+                    if (!whole) {
+                        const float l_other = other_steps > 0 ? peer[0] + peer[kTile] : 0.0f, mb_other = other_steps > 0 ? peer[2 * kTile] : mb;
+                        // (a unit that has seen nothing of the row has a sum of zero, and its offset no say)
+                        top = l_own > 0.0f ? (l_other > 0.0f ? fmaxf(mb, mb_other) : mb) : mb_other;
+                        f_own = l_own > 0.0f ? ptx::ex2_approx(mb - top) : 0.0f;
+                        f_other = l_other > 0.0f ? ptx::ex2_approx(mb_other - top) : 0.0f;
+                        l_row = l_own * f_own + l_other * f_other;
+                    }
+                }
+                const bool joined = seg.part >= 0;  // by combine_kernel
+                if (!joined) {
+                    const float inv = l_row > 0.0f ? 1.0f / l_row : 0.0f;
+                    f_own *= inv;
+                    f_other *= inv;
+                }
+                ptx::tc_fence_after_sync();
+                const int token = tile_first + in_tile, g = row - in_tile * shape.group;
+                const bool alone = whole || tiles == 0;  // a unit's threads have their D / 2 columns; tiles == 0, split: unit 0's
+                const bool stored = in_tile < shape.tile_tokens && token < seg.tokens && (whole || tiles > 0 || q == 0);
+                const int cols = alone ? D / 2 : D / 4;
+                const int col0 = alone ? half * (D / 2) : (q * 2 + half) * (D / 4);
+                const size_t out_row = static_cast<size_t>(seg.token0 + token) * shape.heads + seg.h * shape.group + g;
+                const size_t part_row = static_cast<size_t>(max(seg.part, 0)) * shape.part_rows + token * shape.group + g;
+                if (stored && half == 0 && (whole || q == 0)) {
+                    if (joined)
+                        part_stats[part_row] = make_float2(top, l_row);
+                    else
+                        store_lse(cache, shape, lse, lse2, out_row, seg.q_tile + (whole ? q : 0), seg.h, row, top, l_row);
                 }
                 __syncwarp();
+                const uint32_t o_unit = t_quarter + L::o_col(q), o_peer = t_quarter + L::o_col(q ^ 1);
+                const bool has_own = my_steps > 0, has_other = !whole && other_steps > 0;
+#pragma unroll 1
+                for (int c = col0; c < col0 + cols; c += 16) {
+                    float v[16];
+                    uint32_t o[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                    if (has_own) {
+                        ptx::tmem_ld_32x32b_x16(o_unit + static_cast<uint32_t>(c), o);
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(o[i]) * f_own;
+                    }
+                    if (has_other) {
+                        ptx::tmem_ld_32x32b_x16(o_peer + static_cast<uint32_t>(c), o);
+                        ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = fmaf(__uint_as_float(o[i]), f_other, v[i]);
+                    }
+                    // (no branch around the rest of the loop: the loads of the next columns are the whole warp's)
+                    if (stored && joined) {
+                        float4* dst = reinterpret_cast<float4*>(part_o + part_row * D + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    } else if (stored) {
+                        uint4* dst = reinterpret_cast<uint4*>(O + out_row * D + c);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            dst[i] = make_uint4(ptx::pack_bf16x2(v[8 * i], v[8 * i + 1]), ptx::pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                                                ptx::pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), ptx::pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+                    }
+                    __syncwarp();
+                }
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (!whole && tiles > 0) ptx::mbar_arrive_if(bar_of(offsetof(Barriers, o_free), 0), lane0);
+            }
+            if (tiles > 0) {
+                phases ^= (my_steps & 1) | (my_steps > 0 ? 2u : 0u) | (other_steps > 0 ? 4u : 0u) | (whole ? 8u : 16u);
             }
         }
     }
@@ -675,17 +863,16 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     __syncthreads();
     if (*abort_flag) {
         // Unwinding: let the copies already in flight land before shared memory is released.
-        if (warp == kProducer && lane == 0 && tiles > 0) {
+        if (warp == kProducer && lane == 0) {
             const long long t0 = clock64();
             auto land = [&](uint64_t* full, int stages, int loads) {
                 for (int it = loads > stages ? loads - stages : 0; it < loads; ++it)
                     while (!ptx::mbar_try_wait(&full[it % stages], static_cast<uint32_t>(it / stages) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
                     }
             };
-            land(bars->k_full, L::kKStages, k_loads);
-            land(bars->v_full, v_stages, v_loads);
-            while (!ptx::mbar_try_wait(&bars->q_full, 0) && clock64() - t0 < kWaitLimitCycles / 8) {
-            }
+            land(bars->k_full, L::kStages, k_loads);
+            land(bars->v_full, L::kStages, v_loads);
+            land(bars->q_full, 2, q_loads);
         }
     }
     if (warp == kMma) {
@@ -694,50 +881,113 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     }
 }
 
-// Joins the segments of the rows that were cut: O = sum_s 2^(mb_s - top) O_s / sum_s 2^(mb_s - top) l_s, in the segments' order.  One warp a row.
-constexpr int kJoinWarps = 8;
+// Joins the parts of the blocks that stretches of attn_paged_kernel's CTAs cut: O = sum_s 2^(mb_s - top) O_s / sum_s 2^(mb_s - top) l_s, in the order of
+// the parts.  CTA (c, y): the block that stretch c + 1 begins inside of, if that is its last cut, and of its rows a share.  Where a block has few rows (decoding) several warps take a row's parts in turn.
+constexpr int kJoinWarps = 16;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, const float* part_o, const float2* part_stats,
-               const Plan* plan, __nv_bfloat16* O, float* lse, float* lse2) {
-    __shared__ paged::Samples samples;
-    ptx::grid_dependency_wait();
-    if (*reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u) return;
-    paged::sample_starts(&samples, starts, cache.sequences, kJoinWarps * 32);
-    __syncthreads();
-    const int lane = static_cast<int>(threadIdx.x & 31), warp = static_cast<int>(threadIdx.x >> 5);
-    const long long rows = static_cast<long long>(shape.tokens) * shape.heads;
+               __nv_bfloat16* O, float* lse, float* lse2) {
+    struct Block {
+        int b, h, token0, tokens, q_tile, first, parts;  // the CTA with the first part; parts: of CTAs up to this one, 0: nothing to do here
+    };
     constexpr int kCols = D / 32;
-    for (long long id = static_cast<long long>(blockIdx.x) * kJoinWarps + warp; id < rows; id += static_cast<long long>(gridDim.x) * kJoinWarps) {
-        const int t = static_cast<int>(id / shape.heads), head = static_cast<int>(id % shape.heads);
-        int end;
-        const int b = paged::owner_of(&samples, starts, cache.sequences, t, &end);
-        if (b < 0) continue;
-        const Plan p = plan[b];
-        if (p.segments <= 1) continue;
-        const int i = t - max(starts[b], 0), block = i / (2 * shape.tile_tokens), in_block = i - block * 2 * shape.tile_tokens;
-        const int h = head / shape.group, g = head - h * shape.group;
-        const long long first = p.part + (static_cast<long long>(block) * cache.kv_heads + h) * p.segments * p.rows + in_block * shape.group + g;
-        float top = -3.0e38f, l = 0.0f, v[kCols] = {};
-        for (int s = 0; s < p.segments; ++s) {
-            const long long at = first + static_cast<long long>(s) * p.rows;
-            const float2 st = part_stats[at];
-            if (!(st.y > 0.0f)) continue;
-            const float next = l > 0.0f ? fmaxf(top, st.x) : st.x;
-            const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f = ptx::ex2_approx(st.x - next);
-            top = next;
-            l = l * f_before + st.y * f;
-            const float* src = part_o + at * D + lane * kCols;
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) v[c] = fmaf(src[c], f, v[c] * f_before);
+    __shared__ Block block;
+    __shared__ uint8_t slot_of[256];  // of each part: 0, 1; 2: the CTA has none of the block
+    __shared__ float sums[kJoinWarps][32 * kCols + 2];
+    ptx::grid_dependency_wait();
+    const int lane = static_cast<int>(threadIdx.x & 31), warp = static_cast<int>(threadIdx.x >> 5);
+    const long long cut = static_cast<long long>(blockIdx.x) + 1;
+    if (warp == 0) {
+        Walk walk;
+        walk.find(cache, shape, starts, cut);
+        Block x{};
+        if (walk.b >= 0 && *reinterpret_cast<volatile unsigned int*>(&g_attnw_status) == 0u) {
+            const int all = walk.tiles(shape), here = walk.tiles_before(shape, cut), next = walk.tiles_before(shape, cut + 1);
+            if (here > 0 && here < all && (next >= all || next == 0)) {
+                const int i0 = walk.r * 2 * shape.tile_tokens;
+                x.b = walk.b;
+                x.h = walk.h;
+                x.token0 = min(max(starts[walk.b], 0), shape.tokens) + i0;
+                x.tokens = walk.share.tokens_of(shape, walk.r);
+                x.q_tile = walk.q_tile0 + 2 * walk.r;
+                x.first = static_cast<int>(walk.begin / walk.stretch);
+                x.parts = static_cast<int>(cut) - x.first + 1;
+                for (int i = lane; i < x.parts; i += 32) {
+                    const int t0 = walk.tiles_before(shape, x.first + i), t1 = walk.tiles_before(shape, x.first + i + 1);
+                    slot_of[i] = t0 >= t1 ? 2 : t0 > 0 ? 0 : 1;
+                }
+            }
         }
+        if (lane == 0) block = x;
+    }
+    __syncthreads();
+    const Block x = block;
+    if (x.parts == 0) return;
+    const int rows = x.tokens * shape.group;
+    int each = 1;  // warps a row
+    while (each < kJoinWarps && 2 * each * rows <= kJoinWarps && 4 * each < x.parts) each *= 2;
+    const int per_turn = kJoinWarps / each, mine = warp / each, share = warp % each;
+    for (int r0 = static_cast<int>(blockIdx.y) * per_turn; r0 < rows; r0 += static_cast<int>(gridDim.y) * per_turn) {
+        const int r = r0 + mine;
+        float top = -3.0e38f, l = 0.0f, v[kCols] = {};
+        if (r < rows) {
+            constexpr int kFlight = 4;
+            for (int i0 = share; i0 < x.parts; i0 += kFlight * each) {
+                float2 st[kFlight];
+                float o[kFlight][kCols];
+#pragma unroll
+                for (int f = 0; f < kFlight; ++f) {
+                    const int i = i0 + f * each;
+                    st[f] = make_float2(0.0f, 0.0f);
+                    const int slot = i < x.parts ? slot_of[i] : 2;
+                    if (slot == 2) continue;
+                    const size_t at = static_cast<size_t>(2 * (x.first + i) + slot) * shape.part_rows + r;
+                    st[f] = part_stats[at];
+                    const float* src = part_o + at * D + lane * kCols;
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) o[f][c] = src[c];
+                }
+#pragma unroll
+                for (int f = 0; f < kFlight; ++f) {
+                    if (!(st[f].y > 0.0f)) continue;
+                    const float next = l > 0.0f ? fmaxf(top, st[f].x) : st[f].x;
+                    const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(st[f].x - next);
+                    top = next;
+                    l = l * f_before + st[f].y * f_new;
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) v[c] = fmaf(o[f][c], f_new, v[c] * f_before);
+                }
+            }
+        }
+        if (each > 1) {  // (then there is one turn: rows <= per_turn)
+            sums[warp][32 * kCols] = top;
+            sums[warp][32 * kCols + 1] = l;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = v[c];
+            __syncthreads();
+            if (share > 0) continue;
+            for (int w = warp + 1; w < warp + each; ++w) {
+                const float l_w = sums[w][32 * kCols + 1], top_w = sums[w][32 * kCols];
+                if (!(l_w > 0.0f)) continue;
+                const float next = l > 0.0f ? fmaxf(top, top_w) : top_w;
+                const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(top_w - next);
+                top = next;
+                l = l * f_before + l_w * f_new;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) v[c] = fmaf(sums[w][lane * kCols + c], f_new, v[c] * f_before);
+            }
+        }
+        if (r >= rows) continue;
+        const int token = r / shape.group, g = r - token * shape.group;
+        const size_t out_row = static_cast<size_t>(x.token0 + token) * shape.heads + x.h * shape.group + g;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        __nv_bfloat16* dst = O + static_cast<size_t>(id) * D + lane * kCols;
+        __nv_bfloat16* dst = O + out_row * D + lane * kCols;
 #pragma unroll
         for (int c = 0; c < kCols; c += 2) *reinterpret_cast<uint32_t*>(dst + c) = ptx::pack_bf16x2(v[c] * inv, v[c + 1] * inv);
         if (lane == 0)
-            store_lse(cache, shape, lse, lse2, static_cast<size_t>(id), p.q_tile + i / shape.tile_tokens, h, i % shape.tile_tokens * shape.group + g, top, l);
+            store_lse(cache, shape, lse, lse2, out_row, x.q_tile + token / shape.tile_tokens, x.h, token % shape.tile_tokens * shape.group + g, top, l);
     }
 }
 

@@ -197,10 +197,10 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
 
 // Where the parts of attn_paged's workspace begin.
 struct PagedWorkspace {
-    unsigned long long lse2 = 0, plan = 0, stats = 0, o = 0, bytes = 0;
-    int q_tiles = 0;
-    long long rows = 0;  // of the segments' parts; 0: no block is long enough to be cut
+    unsigned long long lse2 = 0, stats = 0, o = 0, bytes = 0;
+    int q_tiles = 0, part_rows = 0;  // part_rows 0: no block is long enough to be cut
 };
+constexpr int kPagedCtas = 148;  // CTAs of attn_paged_kernel, at most: one an SM of a B200
 PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool weigh) {
     PagedWorkspace w;
     auto take = [&w](unsigned long long bytes) {
@@ -212,11 +212,10 @@ PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool
     w.q_tiles = tokens / tile_tokens + std::min(c->sequences, tokens);
     if (weigh) w.lse2 = take(4ull * kTile * w.q_tiles * c->kv_heads);
     const long long tiles = (static_cast<long long>(c->table_width) * c->page + kTile - 1) / kTile;
-    if (tiles * (tokens > tile_tokens ? 2 : 1) > pa::kLeastCost) {  // (the bound on the rows: pa::schedule)
-        w.rows = 2ll * pa::kSegments * std::min(128ll, static_cast<long long>(tokens) * group);
-        w.plan = take(sizeof(pa::Plan) * static_cast<unsigned long long>(c->sequences));
-        w.stats = take(8ull * w.rows);
-        w.o = take(4ull * w.rows * c->d);
+    if (tiles >= pa::kLeastCut) {  // two parts for each CTA, of a block's rows
+        w.part_rows = static_cast<int>(std::min(2ll * tile_tokens * group, static_cast<long long>(tokens) * group));
+        w.stats = take(8ull * 2 * kPagedCtas * w.part_rows);
+        w.o = take(4ull * 2 * kPagedCtas * w.part_rows * c->d);
     }
     return w;
 }
@@ -240,23 +239,23 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
         return ATTNW_ERR_CUDA;
     }
     const paged::Cache view = view_of(c);
-    const pa::Shape shape{tokens, heads, group, tile_tokens, static_cast<int>(w.rows), w.q_tiles};
+    // As many CTAs as may have something to do: the most that all blocks can cost, by stretches of the least cost.
     const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(std::min(c->sequences, tokens))) * c->kv_heads;
-    const long long grid = blocks + (w.rows > 0 ? pa::kSegments : 0);
-    if (grid > INT_MAX) return ATTNW_ERR_BAD_SHAPE;
-    auto* plan = w.rows > 0 ? reinterpret_cast<pa::Plan*>(workspace + w.plan) : nullptr;
-    auto* stats = w.rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
-    auto* part = w.rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
+    const long long capacity = static_cast<long long>(c->table_width) * c->page, most = blocks * (pa::kBlockCost + capacity * (tokens > tile_tokens ? 2 : 1));
+    const int ctas = static_cast<int>(std::min({static_cast<long long>(kPagedCtas), static_cast<long long>(sm_count), (most + pa::kLeastCost - 1) / pa::kLeastCost}));
+    const pa::Shape shape{tokens, heads, group, tile_tokens, w.part_rows, w.q_tiles, ctas};
+    auto* stats = w.part_rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
+    auto* part = w.part_rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
     const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
     auto* o = static_cast<__nv_bfloat16*>(O);
     auto* lse2 = mass ? reinterpret_cast<float*>(workspace + w.lse2) : nullptr;
-    cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(grid), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
-                                      shape, starts, scale_log2e, o, lse, lse2, part, stats, plan);
+    cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(ctas), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
+                                      shape, starts, scale_log2e, o, lse, lse2, part, stats);
     if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (e == cudaSuccess && plan) {
-        const long long rows = (static_cast<long long>(tokens) * heads + pa::kJoinWarps - 1) / pa::kJoinWarps;
-        e = launch_overlapped(pa::combine_kernel<D>, static_cast<unsigned>(std::min(rows, 8ll * sm_count)), pa::kJoinWarps * 32, 0, stream, 1, view, shape, starts,
-                              part, stats, plan, o, lse, lse2);
+    if (e == cudaSuccess && part && ctas > 1) {
+        const unsigned slices = static_cast<unsigned>((w.part_rows + 4 * pa::kJoinWarps - 1) / (4 * pa::kJoinWarps));
+        e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, starts, part, stats, o,
+                                 lse, lse2);
         if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     if (e == cudaSuccess && mass) {
