@@ -479,6 +479,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     idle_since = 0;
                     continue;
                 }
+                __nanosleep(32);
                 const long long now = clock64();
                 if (idle_since == 0) idle_since = now;
                 bool give_up = *abort_flag != 0u;
@@ -617,7 +618,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const uint32_t t_quarter = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         const uint32_t t_own = t_quarter + L::s_col(q) + static_cast<uint32_t>(half * kHalf);
         const uint32_t o_own = t_quarter + L::o_col(q) + static_cast<uint32_t>(half * (D / 2));  // this thread's D/2 columns of O
-        const float c2 = scale_log2e;
+        const float c2 = fmaxf(scale_log2e, 1.2e-38f);  // (a scale of zero: any finite score counts as zero all the same)
         const uint64_t c2c2 = ptx::pack2(c2, c2);
         const int row = quarter * 32 + lane;
         const int in_tile = row / shape.group;  // the row's token in its query tile
@@ -674,10 +675,11 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&bars->s_free[q]);
-                if (masked) {
+                if (masked) {  // weight zero: c2 > 0 and the offset is finite.  (A branch: few tiles have it.)
+                    asm volatile("" ::: "memory");
 #pragma unroll
                     for (int i = 0; i < kHalf; ++i)
-                        if (i >= valid) s[i] = -3.0e38f;
+                        if (i >= valid) s[i] = __int_as_float(0xff800000);
                 }
                 // ---- row maximum, lazy offset ----
                 float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
@@ -734,10 +736,6 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         ptx::unpack2(ptx::fma2(ptx::pack2(s[g * 8 + i], s[g * 8 + i + 1]), c2c2, nmb2), x0, x1);
                         p[i] = ptx::ex2_approx(x0);
                         p[i + 1] = ptx::ex2_approx(x1);
-                        if (masked) {  // weight zero
-                            p[i] = (g * 8 + i < valid) ? p[i] : 0.0f;
-                            p[i + 1] = (g * 8 + i + 1 < valid) ? p[i + 1] : 0.0f;
-                        }
                         acc[(i >> 1) & 3] = ptx::add2(acc[(i >> 1) & 3], ptx::pack2(p[i], p[i + 1]));
                     }
 #pragma unroll
