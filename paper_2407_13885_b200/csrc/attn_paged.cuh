@@ -165,6 +165,30 @@ __device__ __forceinline__ long long warp_scan(long long x, int lane) {  // incl
     return x;
 }
 
+// (of numbers that are not negative; a division of 64 bits takes a hundred instructions)
+__device__ __forceinline__ long long divided(long long a, long long b) {
+    return (a | b) >> 32 == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
+// How many of a block's key tiles lie in front of stretch `index`: the block begins at `begin`, has `all` tiles, each of 2^shift keys' cost.
+__device__ __forceinline__ int tiles_in_front(long long index, long long stretch, long long begin, int all, int shift) {
+    const long long into = index * stretch - begin - kBlockCost;
+    if (into <= 0) return 0;
+    const long long t = (into + (1ll << shift) - 1) >> shift;
+    if (t >= all) return all;
+    if (all < kLeastCut) return 2 * t < all ? 0 : all;
+    const long long least = max(2ll, stretch >> (5 + shift));  // a shorter part goes to the CTA with the rest
+    return t < least ? 0 : t > all - least ? all : static_cast<int>(t);
+}
+
+// What combine_kernel has to know of a block that was cut, from the CTA that has its last part.
+struct Join {
+    int b, h, token0, tokens, q_tile;
+    int first, parts;  // the CTA with the first part; those from it to the last one's, 0: there is nothing to join
+    int all, shift;    // (tiles_in_front)
+    long long begin, stretch;
+};
+
 // A warp's way along the row of all blocks: sequence by sequence, key head by key head, block by block.  Lane i has the share of sequence
 // b0 + i; everything else is the same in all lanes.
 struct Walk {
@@ -197,7 +221,7 @@ struct Walk {
             total += mine.cost_upto(s, mine.blocks) * c.kv_heads;
         }
         total = warp_sum(total);
-        stretch = max(static_cast<long long>(kLeastCost), (total + s.ctas - 1) / s.ctas);
+        stretch = max(static_cast<long long>(kLeastCost), divided(total + s.ctas - 1, s.ctas));
         const long long at = index * stretch;
         long long first = 0;
         int q_first = 0;
@@ -213,7 +237,7 @@ struct Walk {
                 b = b0 + from;
                 q_tile0 = __shfl_sync(0xffffffffu, q_end - q_tiles, from);
                 const long long seq_begin = __shfl_sync(0xffffffffu, end - cost, from), of_head = __shfl_sync(0xffffffffu, a_head, from);
-                h = static_cast<int>((at - seq_begin) / of_head);
+                h = static_cast<int>(divided(at - seq_begin, of_head));
                 begin = seq_begin + h * of_head;
                 int lo = 0, hi = share.blocks;  // cost_upto(lo) <= at - begin < cost_upto(hi)
                 while (hi - lo > 1) {
@@ -255,16 +279,8 @@ struct Walk {
     }
     __device__ __forceinline__ int weight(const Shape& s) const { return share.tokens_of(s, r) > s.tile_tokens ? 2 : 1; }
     __device__ __forceinline__ int tiles(const Shape& s) const { return (share.seen_of(s, r) + kTile - 1) / kTile; }
-    // How many of the block's key tiles lie in front of stretch `index`.
     __device__ __forceinline__ int tiles_before(const Shape& s, long long index) const {
-        const int all = tiles(s), a_tile = weight(s) * kTile;
-        const long long into = index * stretch - begin - kBlockCost;
-        if (into <= 0) return 0;
-        const long long t = (into + a_tile - 1) / a_tile;
-        if (t >= all) return all;
-        if (all < kLeastCut) return 2 * t < all ? 0 : all;
-        const long long least = max(2ll, stretch / 32 / a_tile);  // a shorter part goes to the CTA with the rest
-        return t < least ? 0 : t > all - least ? all : static_cast<int>(t);
+        return tiles_in_front(index, stretch, begin, tiles(s), weight(s) == 2 ? 8 : 7);
     }
 };
 
@@ -296,7 +312,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, float scale_log2e,
-                  __nv_bfloat16* O, float* lse, float* lse2, float* part_o, float2* part_stats) {
+                  __nv_bfloat16* O, float* lse, float* lse2, float* part_o, float2* part_stats, Join* joins) {
     using L = Smem<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -359,14 +375,17 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     int k_loads = 0, v_loads = 0, q_loads = 0;  // producer: tiles asked for
     // Every role goes through the same segments.  One whose wait has given up goes on without waiting or computing: the Softmax warps' turns
     // need each of them, and a segment's place is free when all have been there.
-    Entry slot;
+    uint32_t segments = 0;  // so far
     bool ok = true;
-    auto segment = [&]() -> const Segment& { return bars->segment[slot.stage]; };
-    auto next_segment = [&]() { return segment_wait(bar_of(offsetof(Barriers, seg_full), slot.stage), slot.phase, abort_flag, kSiteSegment) && segment().b >= 0; };
+    static_assert(kSlots == 4, "two bits of a count, and the parity above them");
+    auto segment = [&]() -> Segment& { return bars->segment[segments & 3u]; };
+    auto next_segment = [&]() {
+        return segment_wait(bar_of(offsetof(Barriers, seg_full), static_cast<int>(segments & 3u)), (segments >> 2) & 1u, abort_flag, kSiteSegment) && segment().b >= 0;
+    };
     auto done_segment = [&]() {
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&bars->seg_free[slot.stage]);
-        slot.next(kSlots);
+        if (lane == 0) ptx::mbar_arrive(&bars->seg_free[segments & 3u]);
+        ++segments;
     };
     // The key tiles of a unit: all of them (whole), or every other one.
     auto steps_of = [&](const Segment& seg, int q) { return seg.whole ? seg.tile1 - seg.tile0 : (seg.tile1 - seg.tile0 + 1 - q) / 2; };
@@ -377,6 +396,15 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         Walk walk;
         const long long cta = blockIdx.x;
         walk.find(cache, shape, starts, cta);
+        Join join{};
+        if (walk.b >= 0 && joins) {  // does the last part of a block lie here that began in front?
+            const int all = walk.tiles(shape), t0 = walk.tiles_before(shape, cta);
+            if (t0 > 0 && t0 < all && walk.tiles_before(shape, cta + 1) >= all) {
+                const int i0 = walk.r * 2 * shape.tile_tokens, first = static_cast<int>(divided(walk.begin, walk.stretch));
+                join = {walk.b, walk.h, min(max(starts[walk.b], 0), shape.tokens) + i0, walk.share.tokens_of(shape, walk.r), walk.q_tile0 + 2 * walk.r,
+                        first, static_cast<int>(cta) - first + 1, all, walk.weight(shape) == 2 ? 8 : 7, walk.begin, walk.stretch};
+            }
+        }
         for (;;) {
             bool more = walk.b >= 0 && walk.begin < (cta + 1) * walk.stretch;
             Segment s{};
@@ -400,15 +428,16 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 walk.next(cache, shape, starts);
                 if (s.b < 0) continue;
             }
-            if (!segment_wait(bar_of(offsetof(Barriers, seg_free), slot.stage), slot.phase ^ 1u, abort_flag, kSiteSegmentFree)) more = false;
+            if (!segment_wait(bar_of(offsetof(Barriers, seg_free), static_cast<int>(segments & 3u)), ((segments >> 2) & 1u) ^ 1u, abort_flag, kSiteSegmentFree)) more = false;
             if (lane == 0) {
-                bars->segment[slot.stage] = s;
-                ptx::mbar_arrive(&bars->seg_full[slot.stage]);
+                segment() = s;
+                ptx::mbar_arrive(&bars->seg_full[segments & 3u]);
             }
             __syncwarp();
-            slot.next(kSlots);
+            ++segments;
             if (!more) break;
         }
+        if (joins && lane == 0) joins[cta] = join;
     } else if (warp == kProducer) {
         // ================= TMA producer: the first keys, Q, then the K and V tiles in the order the MMA issuers read them =========
         // A key tile is up to 8 pages; lane i fetches the part of its page and atom.  Places behind the sequence's length, and pages
@@ -621,9 +650,8 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const float c2 = fmaxf(scale_log2e, 1.2e-38f);  // (a scale of zero: any finite score counts as zero all the same)
         const uint64_t c2c2 = ptx::pack2(c2, c2);
         const int row = quarter * 32 + lane;
-        const int in_tile = row / shape.group;  // the row's token in its query tile
         const uint32_t max_own = ptx::smem_u32(smem + L::kStatOff) + static_cast<uint32_t>((q * 4 * kTile + half * kTile + row) * 4);
-        const uint32_t max_other = ptx::smem_u32(smem + L::kStatOff) + static_cast<uint32_t>((q * 4 * kTile + (half ^ 1) * kTile + row) * 4);
+        static_assert(L::kStatOff % 1024 == 0 && kTile * 4 == 512, "the halves' maxima lie 512 bytes apart, at one bit");
         const uint32_t lane0 = lane == 0;
         const uint32_t p_own = t_quarter + L::p_col(q) + static_cast<uint32_t>(half * 32);  // its 64 keys of P
         // The units take turns at the exponentials (see attn_onepass.cuh); the barrier of a turn is the one that the two threads of a row exchange
@@ -638,8 +666,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const int tiles = seg.tile1 - seg.tile0;
             // The row's token (of the block), and the keys that it sees.  A row that is none's gets what its place would.
             const int tile_first = whole ? q * shape.tile_tokens : 0;  // the first token of this unit's query tile
-            const int seen = min(max(seg.seen0 + tile_first + in_tile, 0), seg.length);
-            const int seen_least = min(max(seg.seen0 + tile_first, 0), seg.length);  // of the tile's rows
+            const int seen = min(max(seg.seen0 + tile_first + row / shape.group, 0), seg.length);
             float smax = -3.0e38f;  // running maximum of the raw scores of this row (all columns)
             float mb = -3.0e38f;    // the offset the weights, l and O's row are relative to (follows smax * c2 lazily)
             float l = 0.0f;         // sum of this thread's weights
@@ -648,7 +675,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (j + 1 - behind < other_steps) ptx::named_arrive(turn_other, 128u);
             };
             const int tile_step = whole ? kTile : 2 * kTile;
-            int tile_begin = key_tile(seg, 0, q) * kTile;
+            int tile_begin = key_tile(seg, 0, q) * kTile + half * kHalf;
             for (int j = 0; j < my_steps; ++j, tile_begin += tile_step) {
                 const uint32_t parity = (phases + static_cast<uint32_t>(j)) & 1u;
                 if (ok) ok = warp_wait(bar_of(offsetof(Barriers, s_full), q), parity, abort_flag, kSiteSFull);
@@ -658,8 +685,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     continue;
                 }
                 ptx::tc_fence_after_sync();
-                const bool masked = seen_least - tile_begin < kTile;  // for some row of the tile
-                const int valid = seen - tile_begin - half * kHalf;   // of this thread's columns
+                const int valid = seen - tile_begin;  // of this thread's columns
                 float s[kHalf];
                 {
                     uint32_t r0[kChunk], r1[kChunk];
@@ -675,7 +701,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&bars->s_free[q]);
-                if (masked) {  // weight zero: c2 > 0 and the offset is finite.  (A branch: few tiles have it.)
+                if (__any_sync(0xffffffffu, valid < kHalf)) {  // weight zero: c2 > 0 and the offset is finite.  (A branch: few tiles have it.)
                     asm volatile("" ::: "memory");
 #pragma unroll
                     for (int i = 0; i < kHalf; ++i)
@@ -701,7 +727,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     pass_turn(j);
                     continue;
                 }
-                smax = ptx::max3(smax, m0, ptx::ld_shared_f32(max_other + place));
+                smax = ptx::max3(smax, m0, ptx::ld_shared_f32((max_own + place) ^ 512u));
                 const float mb_cand = fmaxf(smax * c2, -3.0e38f);
                 const bool move = j == 0 || mb_cand - mb > kLazy;
                 ptx::tc_fence_after_sync();
@@ -798,6 +824,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     f_other *= inv;
                 }
                 ptx::tc_fence_after_sync();
+                const int in_tile = row / shape.group;  // the row's token in its query tile
                 const int token = tile_first + in_tile, g = row - in_tile * shape.group;
                 const bool alone = whole || tiles == 0;  // a unit's threads have their D / 2 columns; tiles == 0, split: unit 0's
                 const bool stored = in_tile < shape.tile_tokens && token < seg.tokens && (whole || tiles > 0 || q == 0);
@@ -880,49 +907,25 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 }
 
 // Joins the parts of the blocks that stretches of attn_paged_kernel's CTAs cut: O = sum_s 2^(mb_s - top) O_s / sum_s 2^(mb_s - top) l_s, in the order of
-// the parts.  CTA (c, y): the block that stretch c + 1 begins inside of, if that is its last cut, and of its rows a share.  Where a block has few rows (decoding) several warps take a row's parts in turn.
+// the parts.  CTA (c, y): the block whose last part CTA c + 1 had, and of its rows a share.  Where a block has few rows (decoding) several warps take a row's parts in turn.
 constexpr int kJoinWarps = 16;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32)
-combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, const float* part_o, const float2* part_stats,
+combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const float* part_o, const float2* part_stats, const Join* joins,
                __nv_bfloat16* O, float* lse, float* lse2) {
-    struct Block {
-        int b, h, token0, tokens, q_tile, first, parts;  // the CTA with the first part; parts: of CTAs up to this one, 0: nothing to do here
-    };
     constexpr int kCols = D / 32;
-    __shared__ Block block;
     __shared__ uint8_t slot_of[256];  // of each part: 0, 1; 2: the CTA has none of the block
     __shared__ float sums[kJoinWarps][32 * kCols + 2];
     ptx::grid_dependency_wait();
     const int lane = static_cast<int>(threadIdx.x & 31), warp = static_cast<int>(threadIdx.x >> 5);
-    const long long cut = static_cast<long long>(blockIdx.x) + 1;
-    if (warp == 0) {
-        Walk walk;
-        walk.find(cache, shape, starts, cut);
-        Block x{};
-        if (walk.b >= 0 && *reinterpret_cast<volatile unsigned int*>(&g_attnw_status) == 0u) {
-            const int all = walk.tiles(shape), here = walk.tiles_before(shape, cut), next = walk.tiles_before(shape, cut + 1);
-            if (here > 0 && here < all && (next >= all || next == 0)) {
-                const int i0 = walk.r * 2 * shape.tile_tokens;
-                x.b = walk.b;
-                x.h = walk.h;
-                x.token0 = min(max(starts[walk.b], 0), shape.tokens) + i0;
-                x.tokens = walk.share.tokens_of(shape, walk.r);
-                x.q_tile = walk.q_tile0 + 2 * walk.r;
-                x.first = static_cast<int>(walk.begin / walk.stretch);
-                x.parts = static_cast<int>(cut) - x.first + 1;
-                for (int i = lane; i < x.parts; i += 32) {
-                    const int t0 = walk.tiles_before(shape, x.first + i), t1 = walk.tiles_before(shape, x.first + i + 1);
-                    slot_of[i] = t0 >= t1 ? 2 : t0 > 0 ? 0 : 1;
-                }
-            }
-        }
-        if (lane == 0) block = x;
+    const Join x = joins[blockIdx.x + 1];
+    if (*reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u || x.parts == 0) return;
+    for (int i = static_cast<int>(threadIdx.x); i < x.parts; i += kJoinWarps * 32) {
+        const int t0 = tiles_in_front(x.first + i, x.stretch, x.begin, x.all, x.shift), t1 = tiles_in_front(x.first + i + 1, x.stretch, x.begin, x.all, x.shift);
+        slot_of[i] = t0 >= t1 ? 2 : t0 > 0 ? 0 : 1;
     }
     __syncthreads();
-    const Block x = block;
-    if (x.parts == 0) return;
     const int rows = x.tokens * shape.group;
     int each = 1;  // warps a row
     while (each < kJoinWarps && 2 * each * rows <= kJoinWarps && 4 * each < x.parts) each *= 2;

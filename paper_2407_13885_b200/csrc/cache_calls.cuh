@@ -197,7 +197,7 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
 
 // Where the parts of attn_paged's workspace begin.
 struct PagedWorkspace {
-    unsigned long long lse2 = 0, stats = 0, o = 0, bytes = 0;
+    unsigned long long lse2 = 0, joins = 0, stats = 0, o = 0, bytes = 0;
     int q_tiles = 0, part_rows = 0;  // part_rows 0: no block is long enough to be cut
 };
 constexpr int kPagedCtas = 148;  // CTAs of attn_paged_kernel, at most: one an SM of a B200
@@ -214,6 +214,7 @@ PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool
     const long long tiles = (static_cast<long long>(c->table_width) * c->page + kTile - 1) / kTile;
     if (tiles >= pa::kLeastCut) {  // two parts for each CTA, of a block's rows
         w.part_rows = static_cast<int>(std::min(2ll * tile_tokens * group, static_cast<long long>(tokens) * group));
+        w.joins = take(sizeof(pa::Join) * kPagedCtas);
         w.stats = take(8ull * 2 * kPagedCtas * w.part_rows);
         w.o = take(4ull * 2 * kPagedCtas * w.part_rows * c->d);
     }
@@ -245,16 +246,17 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
     const int ctas = static_cast<int>(std::min({static_cast<long long>(kPagedCtas), static_cast<long long>(sm_count), (most + pa::kLeastCost - 1) / pa::kLeastCost}));
     const pa::Shape shape{tokens, heads, group, tile_tokens, w.part_rows, w.q_tiles, ctas};
     auto* stats = w.part_rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
+    auto* joins = w.part_rows > 0 ? reinterpret_cast<pa::Join*>(workspace + w.joins) : nullptr;
     auto* part = w.part_rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
     const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
     auto* o = static_cast<__nv_bfloat16*>(O);
     auto* lse2 = mass ? reinterpret_cast<float*>(workspace + w.lse2) : nullptr;
     cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(ctas), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
-                                      shape, starts, scale_log2e, o, lse, lse2, part, stats);
+                                      shape, starts, scale_log2e, o, lse, lse2, part, stats, joins);
     if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && part && ctas > 1) {
         const unsigned slices = static_cast<unsigned>((w.part_rows + 4 * pa::kJoinWarps - 1) / (4 * pa::kJoinWarps));
-        e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, starts, part, stats, o,
+        e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, part, stats, joins, o,
                                  lse, lse2);
         if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     }
