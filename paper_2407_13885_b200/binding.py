@@ -47,6 +47,7 @@ SIGNATURES = {
     "attnw_set_fused_variant": (_int, [_int]),
     "attnw_set_attn_variant": (_int, [_int]),
     "attnw_set_rows_variant": (_int, [_int]),
+    "attnw_set_paged_variant": (_int, [_int]),
     "attnw_launch_count": (_ll, [_int]),
     "attnw_strerror": (ctypes.c_char_p, [_int]),
     "attnw_version": (_int, []),
@@ -130,6 +131,15 @@ def set_attn_variant(variant: str | int) -> None:
     """Selects the kernel behind ``attn_fused``: "auto" (the one-pass kernel), "two_pass" or "one_pass"."""
     code = ATTN_VARIANTS[variant] if isinstance(variant, str) else int(variant)
     _check(lib.attnw_set_attn_variant(code), "attnw_set_attn_variant")
+
+
+PAGED_VARIANTS = {"auto": 0, "tensor_cores": 1, "few": 2}
+
+
+def set_paged_variant(variant: str | int) -> None:
+    """Selects the kernel behind ``attn_paged``: "auto" (by size), "tensor_cores" or "few" (few new tokens)."""
+    code = PAGED_VARIANTS[variant] if isinstance(variant, str) else int(variant)
+    _check(lib.attnw_set_paged_variant(code), "attnw_set_paged_variant")
 
 
 def launch_count(reset: bool = False) -> int:

@@ -27,6 +27,7 @@
 #include "cache_evict.cuh"
 #include "attn_paged.cuh"
 #include "paged_mass.cuh"
+#include "attn_few.cuh"
 
 namespace {
 
@@ -69,6 +70,7 @@ constexpr int kVersion = 100;  // 0.1.0
 std::atomic<long long> g_launches{0};
 std::atomic<int> g_rows_variant{0};   // 0 = tier by row length, 1 = caching (register tier only), 2 = recomputing with a second read, 3 = recomputing from registers
 std::atomic<int> g_attn_variant{0};   // 0 = default (one pass), 1 = two-pass, 2 = one pass
+std::atomic<int> g_paged_variant{0};  // 0 = by size, 1 = tensor cores, 2 = few tokens
 std::atomic<int> g_fused_variant{0};  // 0 = choose by shape, 1 = two-pass, 2 = SRAM-resident, 3 = SRAM-resident, owner-reduce exchange
 constexpr double kTwoPassPerSm = 0.9;  // measured: per-SM throughput of the two-pass kernel relative to the resident one
 std::mutex g_mutex;
@@ -1214,6 +1216,12 @@ int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strid
 int attnw_cache_evict(const attnw_cache* cache, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out,
                       int budget, int recent, void* stream) {
     return evict_entry(cache, table_out, table_out_width, mass, mass_out, kept, lengths_out, budget, recent, stream);
+}
+
+int attnw_set_paged_variant(int variant) {
+    if (variant < 0 || variant > 2) return ATTNW_ERR_BAD_SHAPE;
+    g_paged_variant.store(variant, std::memory_order_relaxed);
+    return ATTNW_OK;
 }
 
 int attnw_set_rows_variant(int variant) {

@@ -276,6 +276,59 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
     return ATTNW_OK;
 }
 
+// How attn_few_kernel would serve a call.
+struct FewShape {
+    int gp = 0;  // heads of the group, rounded up to a power of two; 0: it does not
+    int cluster = 1, max_keys = 0, smem = 0;
+};
+template <int D, int GP>
+constexpr int few_bytes(int max_keys, bool weigh) { return few::Smem<D, GP>::bytes(max_keys, weigh); }
+FewShape few_shape(const attnw_cache* c, int tokens, int heads, bool weigh, int sm_count) {
+    FewShape f;
+    const int group = heads / c->kv_heads;
+    if (group > 8) return f;
+    int gp = 1;
+    while (gp < group) gp *= 2;
+    // A cluster of as many CTAs as fill the device twice, each with 64 keys at least.
+    const long long capacity = static_cast<long long>(c->table_width) * c->page, items = static_cast<long long>(weigh ? c->sequences : tokens) * c->kv_heads;
+    if (items * few::kMaxCluster > INT_MAX) return f;
+    while (f.cluster < few::kMaxCluster && items * f.cluster < 2ll * sm_count && capacity > 64ll * f.cluster) f.cluster *= 2;
+    auto keys_of = [&](int cluster) { return ((capacity + few::kUnit - 1) / few::kUnit + cluster - 1) / cluster * few::kUnit; };
+    while (f.cluster < few::kMaxCluster && keys_of(f.cluster) * (gp + 1) > few::kMaxScores) f.cluster *= 2;
+    if (keys_of(f.cluster) * (gp + 1) > few::kMaxScores) return f;
+    f.max_keys = static_cast<int>(keys_of(f.cluster));
+    f.gp = gp;
+    return f;
+}
+
+template <int D, int GP, bool WEIGH>
+cudaError_t launch_few(const attnw_cache* c, const FewShape& f, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
+                       float* mass_out, int tokens, int heads, float scale, cudaStream_t stream) {
+    constexpr int most = few::Smem<D, GP>::bytes(few::kMaxScores / (GP + 1) / few::kUnit * few::kUnit, WEIGH);
+    cudaError_t e = allow_smem<few::attn_few_kernel<D, GP, WEIGH>>(most);
+    if (e != cudaSuccess) return e;
+    const few::Shape shape{tokens, heads, heads / c->kv_heads, f.cluster, f.max_keys};
+    const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
+    const long long items = static_cast<long long>(WEIGH ? c->sequences : tokens) * c->kv_heads;
+    return launch_overlapped(few::attn_few_kernel<D, GP, WEIGH>, static_cast<unsigned>(items * f.cluster), few::kThreads,
+                             static_cast<size_t>(few::Smem<D, GP>::bytes(f.max_keys, WEIGH)), stream, f.cluster, static_cast<const __nv_bfloat16*>(Q),
+                             tokens > 1 ? q_strides[0] : 0, heads > 1 ? q_strides[1] : 0, view_of(c), shape, starts, scale_log2e, static_cast<__nv_bfloat16*>(O),
+                             lse, mass, mass_out);
+}
+
+template <int D, bool WEIGH>
+cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse,
+                             const float* mass, float* mass_out, int tokens, int heads, float scale, cudaStream_t stream) {
+    const auto launch = f.gp == 1   ? launch_few<D, 1, WEIGH>
+                        : f.gp == 2 ? launch_few<D, 2, WEIGH>
+                        : f.gp == 4 ? launch_few<D, 4, WEIGH>
+                                    : launch_few<D, 8, WEIGH>;
+    return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, stream);
+}
+
+// The most bytes of keys and values (were every cache full) that attn_few_kernel is chosen for.
+constexpr long long kFewBytes = 64ll << 20, kFewBytesWeigh = 256ll << 20;
+
 int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
                 void* workspace, unsigned long long workspace_bytes, int tokens, int heads, float scale, void* stream) {
     int rc = check_cache(c);
@@ -307,6 +360,20 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     DeviceInfo* dev = nullptr;
     rc = current_device(&dev);
     if (rc != ATTNW_OK) return rc;
+    const int variant = g_paged_variant.load(std::memory_order_relaxed);
+    const FewShape f = variant == 1 ? FewShape{} : few_shape(c, tokens, heads, mass != nullptr, dev->sm_count);
+    if (variant == 2 && f.gp == 0) return ATTNW_ERR_UNSUPPORTED;
+    const long long bytes = 4ll * c->d * tokens * c->kv_heads * static_cast<long long>(capacity);
+    if (f.gp > 0 && (variant == 2 || (mass ? bytes <= kFewBytesWeigh && tokens <= c->sequences : bytes <= kFewBytes))) {
+        const auto launch = c->d == 64 ? (mass ? launch_few_group<64, true> : launch_few_group<64, false>)
+                                       : (mass ? launch_few_group<128, true> : launch_few_group<128, false>);
+        if (launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return ATTNW_ERR_CUDA;
+        }
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        return ATTNW_OK;
+    }
     rc = load_encoder();
     if (rc != ATTNW_OK) return rc;
     const auto launch = c->d == 64 ? launch_paged<64> : launch_paged<128>;

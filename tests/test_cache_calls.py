@@ -130,6 +130,13 @@ def test_evict_argument_errors(binding):
     assert f(kept=Y) == 7 and f(lengths_out=0xa000000) == 7 and f(lengths_out=0x5000) == 7
 
 
+def test_paged_variant_knob(binding):
+    lib = binding.lib
+    assert lib.attnw_set_paged_variant(3) == 2 and lib.attnw_set_paged_variant(-1) == 2
+    for v in (1, 2, 0):
+        assert lib.attnw_set_paged_variant(v) == 0
+
+
 def test_workspace_needs_a_cache(binding):
     assert binding.lib.attn_paged_workspace(None, 4, 4, 1) == 0
     assert binding.lib.attn_paged_workspace(cache(binding), 0, 4, 1) == 0

@@ -16,6 +16,13 @@ def attnw():
     assert binding.query_status() == 0
 
 
+@pytest.fixture(params=["auto", "tensor_cores", "few"])
+def variant(attnw, request):
+    attnw.set_paged_variant(request.param)
+    yield request.param
+    attnw.set_paged_variant("auto")
+
+
 # ---- rotary positions ---------------------------------------------------------------------------------------------------------
 
 def rope_tolerance(x, y, frequencies, positions, dtype):
@@ -236,13 +243,15 @@ ATTENTION = [
 
 @pytest.mark.parametrize("H,Hkv,d,page,pairs", ATTENTION)
 @pytest.mark.parametrize("sigma", [1.0, 3.0])
-def test_attention_over_the_cache(attnw, H, Hkv, d, page, pairs, sigma):
+def test_attention_over_the_cache(attnw, variant, H, Hkv, d, page, pairs, sigma):
+    if variant == "few" and H // Hkv > 8:
+        pytest.skip("more heads than it serves")
     c = Paged(pairs, Hkv, d, page, seed=7, front=1, behind=2, sigma=sigma)
     check_attention(attnw, c, c.normal(c.tokens, H, d, sigma=sigma), d ** -0.5)
 
 
 @pytest.mark.parametrize("H,Hkv,d,page,pairs", [ATTENTION[3], ATTENTION[10]])
-def test_attention_with_strided_queries_and_zero_scale(attnw, H, Hkv, d, page, pairs):
+def test_attention_with_strided_queries_and_zero_scale(attnw, variant, H, Hkv, d, page, pairs):
     c = Paged(pairs, Hkv, d, page, seed=3)
     qkv = c.normal(c.tokens, H + 2 * Hkv, d)
     check_attention(attnw, c, qkv[:, :H], 0.1)
@@ -250,7 +259,7 @@ def test_attention_with_strided_queries_and_zero_scale(attnw, H, Hkv, d, page, p
     check_attention(attnw, c, head_major.transpose(0, 1), 0.0, with_mass=False)
 
 
-def test_attention_with_bad_pages_lengths_and_starts(attnw):
+def test_attention_with_bad_pages_lengths_and_starts(attnw, variant):
     c = Paged([(2, 80), (3, 80), (70, 80), (4, 30)], 2, 64, 16, width=5)
     c.table[0, 1], c.table[1, 4], c.table[2, 0] = -1, c.pages, 2 ** 31 - 1   # read as zeros
     c.lengths[3] = -5                                                     # counts as 0
@@ -359,7 +368,7 @@ def test_eviction_ignores_bad_pages(attnw):
 # ---- a run of them together, as generating does ----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("d,Hkv,G", [(64, 3, 4), (128, 2, 1)])
-def test_generating(attnw, d, Hkv, G):
+def test_generating(attnw, variant, d, Hkv, G):
     """Two prompts of different lengths go in by chunks, then some tokens one by one, with an eviction in between: each step's attention is that of the
     definition over the cache as it is, and before the eviction that of attn_fused over the whole sequence for its last token."""
     H, page, budget = Hkv * G, 16, 96
