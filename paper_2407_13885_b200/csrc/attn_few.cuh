@@ -6,8 +6,9 @@
 // memory, turns them into 2^(c s - m) with its own maximum m, adds up the values, and the CTAs join their parts through distributed shared
 // memory.  What a key weighs is then there to be added to `mass`: one launch in all.
 //
-// A warp reads 16 keys at a time (of one page: pages are multiples of 16), D / 8 lanes a key, 16 bytes each; the queries stay in
-// registers; the dot products of a load are reduced over the lanes by halves, heads first, so that GP heads take GP + 1 shuffles (GP > 1) and not 4 GP.
+// A warp reads 8 or 16 keys at a time (of one page: pages are multiples of 16), four 16-byte vectors a lane, and the next ones while it works on
+// them; the queries stay in registers; the dot products are reduced over a key's lanes by halves, heads first, so that 4 heads over 8 lanes
+// take 4 shuffles and not 12.
 // Bound: the latency of a chain of loads (lengths, table, keys, values) for small calls, HBM for large ones.
 #pragma once
 #include "attnw_fused.cuh"
@@ -16,7 +17,7 @@
 namespace attnw {
 namespace few {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnit = 16;          // keys that a warp takes at a time
 constexpr int kMaxCluster = 8;
@@ -38,10 +39,11 @@ struct Smem {
     static constexpr int bytes(int max_keys, bool weigh) { return kScoreOff + max_keys * (GP + (weigh ? 1 : 0)) * 4; }
 };
 
-__device__ __forceinline__ void unpack8(uint4 v, float (&x)[8]) {
+// Eight bfloat16 as four pairs of float32.
+__device__ __forceinline__ void unpack_pairs(uint4 v, uint64_t* x) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) x[i] = ptx::pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
 
 // x[GP], one part in each of LANES neighbouring lanes -> in each lane the whole sum of one: head_of(lane).
@@ -79,14 +81,16 @@ __device__ __forceinline__ int head_of(int lane) {
 
 // Item: without weights (token, key head), with weights (sequence, key head) and its tokens one after the other.
 template <int D, int GP, bool WEIGH>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 1)
 attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape,
                 const int* starts, float scale_log2e, __nv_bfloat16* O, float* lse, const float* mass, float* mass_out) {
     using L = Smem<D, GP>;
-    constexpr int kLanes = D / 8;             // of a key
-    constexpr int kRows = 32 / kLanes;         // keys of a load
-    constexpr int kLoads = kUnit / kRows;      // of a unit
-    constexpr int kHeadLanes = kLanes / GP > 0 ? kLanes / GP : 1;  // lanes that end up with the same sum
+    constexpr int kKeyLanes = GP <= 4 ? 8 : D / 8, kVecs = D / 8 / kKeyLanes;  // keys: lanes of a key, vectors of a lane
+    constexpr int kRowLanes = D / 8;                                            // values: lanes of a key
+    constexpr int kKeys = 4 * (32 / kRowLanes);                                  // that a warp takes at a time, four vectors a lane
+    constexpr int kTurns = kUnit / kKeys;                                        // of a unit
+    constexpr int kHeadLanes = kKeyLanes / GP > 0 ? kKeyLanes / GP : 1;          // lanes that end up with the same sum
+    static_assert(kKeys * kKeyLanes * kVecs == 32 * 4 && kKeyLanes >= GP, "four vectors a lane");
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ paged::Samples samples;
     float* part = reinterpret_cast<float*>(smem + L::kPartOff);
@@ -135,67 +139,76 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
     }
     // (A peer's shared memory is written to only when the peer runs: the other half of this is in front of the first such store.)
     if (S > 1 && t0 < t1) ptx::cluster_arrive_relaxed();
-    const int column = lane % kLanes, of_load = lane / kLanes;  // this lane's 8 features, and its key of a load
     // The pages of this warp's first 32 units, one a lane; -1: none that the cache has.
     const int my_first = unit0 + warp + kWarps * lane;
     const int page_mine = my_first < unit1 ? paged::page_of(cache.table, cache, b, my_first * kUnit) : -1;
-    // A unit's rows, as 16-byte vectors: zeros where there is no key that the token sees, or no page.
-    auto fetch = [&](const __nv_bfloat16* data, int i, int seen, uint4 (&v)[kLoads]) {
-        const int unit = unit0 + warp + kWarps * i;
-        const int page = i < 32 ? __shfl_sync(0xffffffffu, page_mine, i & 31) : unit < unit1 ? paged::page_of(cache.table, cache, b, unit * kUnit) : -1;
-        const __nv_bfloat16* rows = data + (page >= 0 ? paged::row_offset(cache, page, h, unit * kUnit) : 0) + column * 8;
+    // Turn i of this warp: kKeys keys as four vectors a lane, `lanes` lanes a key; zeros where there is no key that the token sees, or no page.
+    auto fetch = [&](const __nv_bfloat16* data, int i, int seen, int lanes, uint4 (&v)[4]) {
+        const int n = i / kTurns, unit = unit0 + warp + kWarps * n;
+        const int page = n < 32 ? __shfl_sync(0xffffffffu, page_mine, n & 31) : unit < unit1 ? paged::page_of(cache.table, cache, b, unit * kUnit) : -1;
+        const int key = unit * kUnit + i % kTurns * kKeys;
+        const __nv_bfloat16* rows = data + (page >= 0 ? paged::row_offset(cache, page, h, key) : 0);
+        const int vecs = D / 8 / lanes;
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const int row = n * kRows + of_load;
-            v[n] = page >= 0 && unit * kUnit + row < seen ? __ldcs(reinterpret_cast<const uint4*>(rows + static_cast<size_t>(row) * D)) : make_uint4(0u, 0u, 0u, 0u);
+        for (int x = 0; x < 4; ++x) {
+            const int row = x / vecs * (32 / lanes) + lane / lanes, column = x % vecs * lanes + lane % lanes;
+            v[x] = page >= 0 && key + row < seen ? __ldcs(reinterpret_cast<const uint4*>(rows + row * D + column * 8)) : make_uint4(0u, 0u, 0u, 0u);
         }
     };
-    const int my_units = (unit1 - unit0 - warp + kWarps - 1) / kWarps;  // of this warp (0 or less: none)
+    const int my_turns = max(0, unit1 - unit0 - warp + kWarps - 1) / kWarps * kTurns;  // of this warp
+    auto turn_begin = [&](int i) { return (warp + kWarps * (i / kTurns)) * kUnit + i % kTurns * kKeys; };  // its first key, from key0 on
     const float c2 = scale_log2e;
 
     for (int t = t0; t < t1; ++t) {
         const long long seen_by = static_cast<long long>(length) - (static_cast<long long>(end) - t) + 1;
         const int seen = static_cast<int>(min(max(seen_by, 0ll), static_cast<long long>(length)));
-        float q[GP][8];
+        uint64_t q[GP][4 * kVecs];  // pairs of features
 #pragma unroll
-        for (int g = 0; g < GP; ++g) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (g < shape.group) v = *reinterpret_cast<const uint4*>(Q + t * q_token + (h * shape.group + g) * q_head + column * 8);
-            unpack8(v, q[g]);
-        }
+        for (int g = 0; g < GP; ++g)
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (g < shape.group)
+                    v = *reinterpret_cast<const uint4*>(Q + t * q_token + (h * shape.group + g) * q_head + (i * kKeyLanes + lane % kKeyLanes) * 8);
+                unpack_pairs(v, q[g] + 4 * i);
+            }
         // ---- scores, and their maximum ----
-        const int head = head_of<GP, kLanes>(lane);
+        const int head = head_of<GP, kKeyLanes>(lane);
         float top = -3.0e38f;
-        for (int i = 0; i < my_units; ++i) {
-            uint4 v[kLoads];
-            fetch(cache.K, i, seen, v);
-            const int at = (warp + kWarps * i) * kUnit;  // the unit's first key, from key0 on
+        uint4 next[4];
+        if (my_turns > 0) fetch(cache.K, 0, seen, kKeyLanes, next);
+        for (int i = 0; i < my_turns; ++i) {
+            uint4 v[4];
 #pragma unroll
-            for (int n = 0; n < kLoads; ++n) {
-                float k[8], dot[GP];
-                unpack8(v[n], k);
+            for (int x = 0; x < 4; ++x) v[x] = next[x];
+            if (i + 1 < my_turns) fetch(cache.K, i + 1, seen, kKeyLanes, next);
+            const int at = turn_begin(i) + lane / kKeyLanes;
+#pragma unroll
+            for (int x = 0; x < 4; x += kVecs) {
+                uint64_t k[4 * kVecs];
+#pragma unroll
+                for (int y = 0; y < kVecs; ++y) unpack_pairs(v[x + y], k + 4 * y);
+                float dot[GP];
 #pragma unroll
                 for (int g = 0; g < GP; ++g) {
-                    uint64_t sum = ptx::mul2(ptx::pack2(q[g][0], q[g][1]), ptx::pack2(k[0], k[1]));
+                    uint64_t sum = ptx::mul2(q[g][0], k[0]);
 #pragma unroll
-                    for (int e = 2; e < 8; e += 2) sum = ptx::fma2(ptx::pack2(q[g][e], q[g][e + 1]), ptx::pack2(k[e], k[e + 1]), sum);
-                    float a, b2;
-                    ptx::unpack2(sum, a, b2);
-                    dot[g] = a + b2;
+                    for (int e = 1; e < 4 * kVecs; ++e) sum = ptx::fma2(q[g][e], k[e], sum);
+                    float lo, hi;
+                    ptx::unpack2(sum, lo, hi);
+                    dot[g] = lo + hi;
                 }
-                const float z = reduce_heads<GP, kLanes>(dot, lane);
-                const int key = at + n * kRows + of_load;
-                const float s = key0 + key < seen ? z * c2 : __int_as_float(0xff800000);
+                const int key = at + x / kVecs * (32 / kKeyLanes);
+                const float z = reduce_heads<GP, kKeyLanes>(dot, lane), s = key0 + key < seen ? z * c2 : __int_as_float(0xff800000);
                 top = fmaxf(top, s);
                 if (lane % kHeadLanes == 0) scores[key * GP + head] = s;
             }
         }
         // the first values are on their way while the scores are turned into weights
-        uint4 first_v[kLoads];
-        if (my_units > 0) fetch(cache.V, 0, seen, first_v);
-        if (kRows > 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-        if (kRows > 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-        if (lane < kLanes && lane % kHeadLanes == 0) of_warps[warp * GP + head] = top;
+        if (my_turns > 0) fetch(cache.V, 0, seen, kRowLanes, next);
+#pragma unroll
+        for (int o = 16; o >= kKeyLanes; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane < kKeyLanes && lane % kHeadLanes == 0) of_warps[warp * GP + head] = top;
         __syncthreads();
         // ---- weights relative to this CTA's maxima, and their sums ----
         float m[GP], l[GP];
@@ -237,41 +250,46 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
             }
         }
         // ---- values ----
-        float o[GP][8] = {};
-        for (int i = 0; i < my_units; ++i) {
-            uint4 v[kLoads];
-            if (i == 0) {
+        uint64_t o2[GP][4];
 #pragma unroll
-                for (int n = 0; n < kLoads; ++n) v[n] = first_v[n];
-            } else {
-                fetch(cache.V, i, seen, v);
-            }
-            const int at = (warp + kWarps * i) * kUnit;
+        for (int g = 0; g < GP; ++g)
 #pragma unroll
-            for (int n = 0; n < kLoads; ++n) {
-                float x[8];
-                unpack8(v[n], x);
-                const float* p = scores + (at + n * kRows + of_load) * GP;
+            for (int e = 0; e < 4; ++e) o2[g][e] = 0ull;
+        for (int i = 0; i < my_turns; ++i) {
+            uint4 v[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] = next[x];
+            if (i + 1 < my_turns) fetch(cache.V, i + 1, seen, kRowLanes, next);
+            const float* p = scores + (turn_begin(i) + lane / kRowLanes) * GP;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                uint64_t y[4];
+                unpack_pairs(v[x], y);
 #pragma unroll
                 for (int g = 0; g < GP; ++g) {
-                    const uint64_t pp = ptx::pack2(p[g], p[g]);
+                    const float w = p[x * (32 / kRowLanes) * GP + g];
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2)
-                        ptx::unpack2(ptx::fma2(pp, ptx::pack2(x[e], x[e + 1]), ptx::pack2(o[g][e], o[g][e + 1])), o[g][e], o[g][e + 1]);
+                    for (int e = 0; e < 4; ++e) o2[g][e] = ptx::fma2(ptx::pack2(w, w), y[e], o2[g][e]);
                 }
             }
         }
+        float o[GP][8];
 #pragma unroll
         for (int g = 0; g < GP; ++g)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (kRows > 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], 16);
-                if (kRows > 2) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], 8);
+                if (e % 2 == 0) ptx::unpack2(o2[g][e / 2], o[g][e], o[g][e + 1]);
             }
-        if (lane < kLanes)
+#pragma unroll
+        for (int g = 0; g < GP; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int x = 16; x >= kRowLanes; x >>= 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], x);
+        if (lane < kRowLanes)
 #pragma unroll
             for (int g = 0; g < GP; ++g) {
-                float4* dst = reinterpret_cast<float4*>(part + (warp * GP + g) * D + column * 8);
+                float4* dst = reinterpret_cast<float4*>(part + (warp * GP + g) * D + lane * 8);
                 dst[0] = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
                 dst[1] = make_float4(o[g][4], o[g][5], o[g][6], o[g][7]);
             }

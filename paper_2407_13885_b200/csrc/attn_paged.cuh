@@ -121,7 +121,7 @@ struct Shape {
 
 // A sequence's blocks.
 struct Share {
-    int n, seen0, length, blocks;  // new tokens, (see Segment), blocks a key head
+    int n, token0, seen0, length, blocks;  // new tokens, the first of them, (see Segment), blocks a key head
 
     __device__ __forceinline__ int tokens_of(const Shape& s, int r) const { return min(n - r * 2 * s.tile_tokens, 2 * s.tile_tokens); }
     __device__ __forceinline__ int seen_of(const Shape& s, int r) const {  // keys that block r's last token sees
@@ -144,6 +144,7 @@ __device__ __forceinline__ Share share_of(const paged::Cache& c, const Shape& s,
     const int s0 = starts[b], s1 = starts[b + 1];
     const int t0 = min(max(s0, 0), s.tokens), t1 = min(max(s1, 0), s.tokens);
     r.n = max(t1 - t0, 0);
+    r.token0 = t0;
     r.length = paged::length_of(c, b);
     const long long seen = static_cast<long long>(r.length) - (static_cast<long long>(s1) - t0) + 1;
     r.seen0 = static_cast<int>(min(max(seen, -(1ll << 30)), 1ll << 30));
@@ -206,6 +207,7 @@ struct Walk {
     }
     __device__ __forceinline__ void take(int from) {  // the share of lane `from`
         share.n = __shfl_sync(0xffffffffu, mine.n, from);
+        share.token0 = __shfl_sync(0xffffffffu, mine.token0, from);
         share.seen0 = __shfl_sync(0xffffffffu, mine.seen0, from);
         share.length = __shfl_sync(0xffffffffu, mine.length, from);
         share.blocks = __shfl_sync(0xffffffffu, mine.blocks, from);
@@ -397,25 +399,22 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const long long cta = blockIdx.x;
         walk.find(cache, shape, starts, cta);
         Join join{};
-        if (walk.b >= 0 && joins) {  // does the last part of a block lie here that began in front?
-            const int all = walk.tiles(shape), t0 = walk.tiles_before(shape, cta);
-            if (t0 > 0 && t0 < all && walk.tiles_before(shape, cta + 1) >= all) {
-                const int i0 = walk.r * 2 * shape.tile_tokens, first = static_cast<int>(divided(walk.begin, walk.stretch));
-                join = {walk.b, walk.h, min(max(starts[walk.b], 0), shape.tokens) + i0, walk.share.tokens_of(shape, walk.r), walk.q_tile0 + 2 * walk.r,
-                        first, static_cast<int>(cta) - first + 1, all, walk.weight(shape) == 2 ? 8 : 7, walk.begin, walk.stretch};
-            }
-        }
+        bool first_block = true;
         for (;;) {
             bool more = walk.b >= 0 && walk.begin < (cta + 1) * walk.stretch;
             Segment s{};
             s.b = -1;
             if (more) {
                 const int all = walk.tiles(shape), t0 = walk.tiles_before(shape, cta), t1 = walk.tiles_before(shape, cta + 1);
+                const int i0 = walk.r * 2 * shape.tile_tokens;
+                if (first_block && t0 > 0 && t0 < t1 && t1 == all)  // the last part of a block that began in front
+                    join = {walk.b, walk.h, walk.share.token0 + i0, walk.share.tokens_of(shape, walk.r), walk.q_tile0 + 2 * walk.r,
+                            -1, 0, all, walk.weight(shape) == 2 ? 8 : 7, walk.begin, walk.stretch};
+                first_block = false;
                 if (t0 < t1 || (all == 0 && walk.begin >= cta * walk.stretch)) {
-                    const int i0 = walk.r * 2 * shape.tile_tokens;
                     s.b = walk.b;
                     s.h = walk.h;
-                    s.token0 = min(max(starts[walk.b], 0), shape.tokens) + i0;
+                    s.token0 = walk.share.token0 + i0;
                     s.tokens = walk.share.tokens_of(shape, walk.r);
                     s.seen0 = walk.share.seen0 + i0;
                     s.length = walk.share.length;
@@ -425,19 +424,27 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     s.q_tile = walk.q_tile0 + 2 * walk.r;
                     s.part = t1 - t0 == all ? -1 : 2 * static_cast<int>(cta) + (t0 > 0 ? 0 : 1);
                 }
-                walk.next(cache, shape, starts);
-                if (s.b < 0) continue;
             }
-            if (!segment_wait(bar_of(offsetof(Barriers, seg_free), static_cast<int>(segments & 3u)), ((segments >> 2) & 1u) ^ 1u, abort_flag, kSiteSegmentFree)) more = false;
-            if (lane == 0) {
-                segment() = s;
-                ptx::mbar_arrive(&bars->seg_full[segments & 3u]);
+            if (!more || s.b >= 0) {
+                if (!segment_wait(bar_of(offsetof(Barriers, seg_free), static_cast<int>(segments & 3u)), ((segments >> 2) & 1u) ^ 1u, abort_flag, kSiteSegmentFree))
+                    more = false;
+                if (lane == 0) {
+                    segment() = s;
+                    ptx::mbar_arrive(&bars->seg_full[segments & 3u]);
+                }
+                __syncwarp();
+                ++segments;
             }
-            __syncwarp();
-            ++segments;
             if (!more) break;
+            walk.next(cache, shape, starts);
         }
-        if (joins && lane == 0) joins[cta] = join;
+        if (joins && lane == 0) {
+            if (join.all > 0) {
+                join.first = static_cast<int>(divided(join.begin, join.stretch));
+                join.parts = static_cast<int>(cta) - join.first + 1;
+            }
+            joins[cta] = join;
+        }
     } else if (warp == kProducer) {
         // ================= TMA producer: the first keys, Q, then the K and V tiles in the order the MMA issuers read them =========
         // A key tile is up to 8 pages; lane i fetches the part of its page and atom.  Places behind the sequence's length, and pages
@@ -484,20 +491,25 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             // Both kinds in the order of the keys (split: the units take them in turn), each as soon as it has room.
             int k = 0, v = 0, where_k = place(tile0), where_v = where_k;
             long long idle_since = 0;
+            bool q_here = false;
+            auto ready = [&](size_t barrier, const Entry& e) { return __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(barrier, e.stage), e.phase ^ 1u)); };
+            auto load_queries = [&]() {
+                load_q(0);
+                if (seg.whole) load_q(1);
+                q_here = true;
+            };
+            if (ready(offsetof(Barriers, q_free), eq)) load_queries();  // (beside the table's answer)
             while (ok && v < tiles) {
                 bool idle = true;
-                if (k < tiles && __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(offsetof(Barriers, k_empty), ek.stage), ek.phase ^ 1u))) {
+                if (k < tiles && ready(offsetof(Barriers, k_empty), ek)) {
                     load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), smem + L::kKOff + ek.stage * L::kTileBytes, tile0 + k, where_k);
                     ek.next(L::kStages);
                     ++k_loads;
-                    if (k == 0) {
-                        load_q(0);
-                        if (seg.whole) load_q(1);
-                    }
+                    if (!q_here) load_queries();
                     where_k = place(tile0 + ++k);
                     idle = false;
                 }
-                if (ok && v < k && __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(offsetof(Barriers, v_empty), ev.stage), ev.phase ^ 1u))) {
+                if (ok && v < k && ready(offsetof(Barriers, v_empty), ev)) {
                     load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), smem + L::kVOff + ev.stage * L::kTileBytes, tile0 + v, where_v);
                     ev.next(L::kStages);
                     ++v_loads;

@@ -289,12 +289,12 @@ FewShape few_shape(const attnw_cache* c, int tokens, int heads, bool weigh, int 
     if (group > 8) return f;
     int gp = 1;
     while (gp < group) gp *= 2;
-    // A cluster of as many CTAs as fill the device twice, each with 64 keys at least.
+    // A cluster of as many CTAs as fill the device once, each with 64 keys at least.
     const long long capacity = static_cast<long long>(c->table_width) * c->page, items = static_cast<long long>(weigh ? c->sequences : tokens) * c->kv_heads;
     if (items * few::kMaxCluster > INT_MAX) return f;
-    while (f.cluster < few::kMaxCluster && items * f.cluster < 2ll * sm_count && capacity > 64ll * f.cluster) f.cluster *= 2;
+    f.cluster = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(few::kMaxCluster), sm_count / items, capacity / 64})));
     auto keys_of = [&](int cluster) { return ((capacity + few::kUnit - 1) / few::kUnit + cluster - 1) / cluster * few::kUnit; };
-    while (f.cluster < few::kMaxCluster && keys_of(f.cluster) * (gp + 1) > few::kMaxScores) f.cluster *= 2;
+    while (f.cluster < few::kMaxCluster && keys_of(f.cluster) * (gp + 1) > few::kMaxScores) ++f.cluster;
     if (keys_of(f.cluster) * (gp + 1) > few::kMaxScores) return f;
     f.max_keys = static_cast<int>(keys_of(f.cluster));
     f.gp = gp;
@@ -326,8 +326,20 @@ cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void
     return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, stream);
 }
 
-// The most bytes of keys and values (were every cache full) that attn_few_kernel is chosen for.
-constexpr long long kFewBytes = 64ll << 20, kFewBytesWeigh = 256ll << 20;
+// Is it the faster one?  Its time goes by the bytes that an SM reads, 27 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
+// other one's by the bytes in all, which it spreads evenly, after 12 us (one wave of short blocks) to 25 (cut ones, joined), and with weights 20
+// more.  The lengths are on the device: caches count as full.  us per call, few -> tensor cores, 32 heads on 8, d = 128: one token over 100 keys 7.3 / 12.6,
+// 1000 8.9 / 24.7, 4000 13.1 / 24.2, 16000 33.6 / 26.5, 4 over 4000 21.2 / 27.8, 16 over 1000 20.1 / 26.9, 16 tokens of one sequence over 500
+// 20.2 / 17.5; 64 heads on 8, 8 tokens over 4000 72 / 42; 8 heads on 8 31 / 42.  With weights: 1 over 1000 10.3 / 36.2, 16000 35 / 48, 32 over 4095 145 / 202, 64
+// heads on 8, 8 over 4000 81 / 75; four tokens of one sequence over 100 27 / 23.
+bool few_pays(const attnw_cache* c, const FewShape& f, int tokens, bool weigh, int sm_count) {
+    if (weigh && tokens > c->sequences) return false;  // (a sequence's tokens take turns there)
+    const long long ctas = static_cast<long long>(weigh ? c->sequences : tokens) * c->kv_heads * f.cluster, waves = (ctas + sm_count - 1) / sm_count;
+    long long most = f.gp <= 2 ? 1024 : f.gp == 4 ? 512 : 256;  // kB
+    if (weigh) most = f.gp <= 4 ? 4096 : 768;
+    if (tokens > c->sequences) most /= 2;
+    return waves * (f.max_keys * 4ll * c->d / 1024 + 128) <= most + 128;
+}
 
 int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
                 void* workspace, unsigned long long workspace_bytes, int tokens, int heads, float scale, void* stream) {
@@ -363,8 +375,7 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     const int variant = g_paged_variant.load(std::memory_order_relaxed);
     const FewShape f = variant == 1 ? FewShape{} : few_shape(c, tokens, heads, mass != nullptr, dev->sm_count);
     if (variant == 2 && f.gp == 0) return ATTNW_ERR_UNSUPPORTED;
-    const long long bytes = 4ll * c->d * tokens * c->kv_heads * static_cast<long long>(capacity);
-    if (f.gp > 0 && (variant == 2 || (mass ? bytes <= kFewBytesWeigh && tokens <= c->sequences : bytes <= kFewBytes))) {
+    if (f.gp > 0 && (variant == 2 || few_pays(c, f, tokens, mass != nullptr, dev->sm_count))) {
         const auto launch = c->d == 64 ? (mass ? launch_few_group<64, true> : launch_few_group<64, false>)
                                        : (mass ? launch_few_group<128, true> : launch_few_group<128, false>);
         if (launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
