@@ -10,6 +10,7 @@
 // keys' way from HBM.
 #pragma once
 #include <cstddef>
+#include <type_traits>
 
 #include "attn_paged.cuh"
 
@@ -20,7 +21,7 @@ constexpr int kThreads = 576;
 constexpr int kSmWarps = 16;  // unit (2) x half of the columns (2) x TMEM lane quarter (4)
 constexpr int kProducer = 16;
 constexpr int kMma = 17;
-constexpr int kSegments = 444;  // about as many segments are wanted in all: three an SM of a B200
+constexpr int kSegments = 148;  // about as many segments are wanted in all, of the same cost: one an SM of a B200
 
 enum : uint32_t {  // wait sites
     kSiteKEmpty = 80,
@@ -37,12 +38,14 @@ struct Smem {
     static constexpr int kAtoms = D / 64;
     static constexpr int kAtomBytes = kTile * 128;
     static constexpr int kTileBytes = kAtoms * kAtomBytes;
-    static constexpr int kPairs = 2;  // pairs of key tiles in flight
-    static constexpr int kQStages = (D == 128) ? 2 : 4;
-    static constexpr int kKOff = 0;
-    static constexpr int kQOff = kKOff + kPairs * 2 * kTileBytes;
-    static constexpr int kLseOff = kQOff + kQStages * kTileBytes;  // float [stage][128]
-    static constexpr int kSumOff = kLseOff + kQStages * kTile * 4;  // float [pair parity][unit][half][128]
+    // Six places for tiles.  One query tile: two pairs of key tiles, and it.  More: one pair, and four query tiles on their way (with two a tile of
+    // 2 x 128 x 128 waited 0.9 us for the next one).
+    static constexpr int kPlaces = 6;
+    static __device__ __forceinline__ int pairs(bool resident) { return resident ? 2 : 1; }
+    static __device__ __forceinline__ int q_stages(bool resident) { return resident ? 1 : 4; }
+    static __device__ __forceinline__ int q_offset(bool resident, int stage) { return ((resident ? 4 : 2) + stage) * kTileBytes; }
+    static constexpr int kLseOff = kPlaces * kTileBytes;            // float [stage][128]
+    static constexpr int kSumOff = kLseOff + 4 * kTile * 4;  // float [pair parity][unit][half][128]
     static constexpr int kBarOff = kSumOff + 2 * 2 * 2 * kTile * 4;
     static constexpr int kBytes = kBarOff + 512;
     static constexpr int kDynamicBytes = kBytes + 1024;
@@ -67,7 +70,7 @@ struct Barriers {
 };
 static_assert(sizeof(Barriers) <= 512, "barrier block must fit its slot");
 
-// By one warp.  A segment is a number of pairs of key tiles; its cost is that of their score tiles, and about one more a key tile for itself.
+// By one warp.  A segment is a number of pairs of key tiles; a key tile's cost is that of its score tiles, and about one more for itself.
 __device__ __noinline__ void schedule(const paged::Cache& c, const pa::Shape& s, const int* starts, int index, Segment* out) {
     const int lane = static_cast<int>(threadIdx.x & 31);
     auto cost_of = [&](const pa::Share& r) { return static_cast<long long>((r.n + s.tile_tokens - 1) / s.tile_tokens) + 1; };  // of a key tile
@@ -77,7 +80,7 @@ __device__ __noinline__ void schedule(const paged::Cache& c, const pa::Shape& s,
         if (r.n > 0) total += cost_of(r) * ((r.length + kTile - 1) / kTile) * c.kv_heads;
     }
     total = pa::warp_sum(total);
-    const long long most = (total + kSegments - 1) / kSegments;
+    const long long most = max(1ll, (total + total / 16 + kSegments - 1) / kSegments);  // (a little more: what does not fit one round of CTAs takes another)
     long long first = 0, q_first = 0;
     if (lane == 0) out->b = -1;
     __syncwarp();
@@ -86,8 +89,9 @@ __device__ __noinline__ void schedule(const paged::Cache& c, const pa::Shape& s,
         pa::Share r{};
         if (b < c.sequences) r = pa::share_of(c, s, starts, b);
         const int tiles = r.n > 0 ? (r.length + kTile - 1) / kTile : 0;
-        const long long each = 2 * max(1ll, (most + 2 * cost_of(r) - 1) / (2 * cost_of(r)));  // key tiles of a segment; they cost `most` or more
-        const long long segments = (tiles + each - 1) / each;
+        // As many as come nearest to that cost, of an even number of key tiles each.
+        const long long wanted = max(1ll, (tiles * cost_of(r) + most / 2) / most), each = (tiles + 2 * wanted - 1) / (2 * wanted) * 2;
+        const long long segments = tiles > 0 ? (tiles + each - 1) / each : 0;
         const long long end = first + pa::warp_scan(segments * c.kv_heads, lane), begin = end - segments * c.kv_heads;
         const long long q_tiles = (r.n + s.tile_tokens - 1) / s.tile_tokens, q_end = q_first + pa::warp_scan(q_tiles, lane);
         if (index >= begin && index < end) {
@@ -124,11 +128,11 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 
     // ---- set-up ------------------------------------------------------------------------------
     if (warp == kProducer && lane == 0) {
-        for (int s = 0; s < L::kPairs; ++s) {
+        for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(&bars->k_full[s], 1);
             ptx::mbar_init(&bars->k_empty[s], 1);
         }
-        for (int s = 0; s < L::kQStages; ++s) {
+        for (int s = 0; s < 4; ++s) {
             ptx::mbar_init(&bars->q_full[s], 1);
             ptx::mbar_init(&bars->q_empty[s], 1 + kSmWarps);
         }
@@ -159,6 +163,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     const int q_tiles = (seg.tokens + shape.tile_tokens - 1) / shape.tile_tokens;
     const int pairs = seg.b < 0 ? 0 : (seg.tile1 - seg.tile0 + 1) / 2;
     const bool resident = q_tiles == 1;
+    const int k_stages = L::pairs(resident), q_stages = L::q_stages(resident);
     auto t_first = [&](int kt) { return max(kt * kTile - seg.seen0 + 1, 0) / shape.tile_tokens; };  // q_tiles or more: nobody sees it
     struct Entry {  // of a ring
         int stage = 0;
@@ -194,14 +199,14 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 const uint32_t full = bar_of(offsetof(Barriers, q_full), eq.stage);
                 ptx::mbar_expect_tx(full, static_cast<uint32_t>(q_bytes + kTile * 4));
                 for (int a = 0; a < L::kAtoms; ++a)
-                    ptx::tma_load_4d(smem + L::kQOff + eq.stage * L::kTileBytes + a * L::kAtomBytes, &tm_q, &bars->q_full[eq.stage], a * 64, 0, seg.h,
+                    ptx::tma_load_4d(smem + L::q_offset(resident, eq.stage) + a * L::kAtomBytes, &tm_q, &bars->q_full[eq.stage], a * 64, 0, seg.h,
                                      seg.token0 + t * shape.tile_tokens);
                 ptx::bulk_load_1d(ptx::smem_u32(smem + L::kLseOff + eq.stage * kTile * 4),
                                   lse2 + (static_cast<size_t>(min(seg.q_tile + t, shape.q_tiles - 1)) * cache.kv_heads + seg.h) * kTile, kTile * 4,
                                   &bars->q_full[eq.stage]);
             }
             __syncwarp();
-            eq.next(L::kQStages);
+            eq.next(q_stages);
             ++q_loads;
         };
         for (int p = 0; ok && p < pairs; ++p) {
@@ -217,10 +222,10 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             __syncwarp();
             if (fetches)
                 for (int u = 0; u < (both ? 2 : 1); ++u)
-                    ptx::tma_load_3d(smem + L::kKOff + (2 * ek.stage + u) * L::kTileBytes + atom * L::kAtomBytes + (part << page_shift) * 128, &tm_k, full, atom * 64,
+                    ptx::tma_load_3d(smem + (2 * ek.stage + u) * L::kTileBytes + atom * L::kAtomBytes + (part << page_shift) * 128, &tm_k, full, atom * 64,
                                      ((kt + u) * kTile) & ((1 << cache.page_shift) - 1) & ~(kTile - 1), where[u], keep);
             __syncwarp();
-            ek.next(L::kPairs);
+            ek.next(k_stages);
             ++k_loads;
             if (!resident)
                 for (int t = t0; ok && t < q_tiles; ++t) load_q(t);
@@ -248,8 +253,8 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (!ok) break;
                     ++uses[u];
                     ptx::tc_fence_after_sync();
-                    const uint64_t a_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(L::kKOff + (2 * ek.stage + u) * L::kTileBytes));
-                    const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(L::kQOff + eq.stage * L::kTileBytes));
+                    const uint64_t a_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>((2 * ek.stage + u) * L::kTileBytes));
+                    const uint64_t b_desc = ptx::umma_desc_kmajor_sw128(base + static_cast<uint32_t>(L::q_offset(resident, eq.stage)));
                     if (ptx::elect_one()) {
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
@@ -264,13 +269,13 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 if (!resident) {
                     if (ptx::elect_one()) ptx::umma_commit(&bars->q_empty[eq.stage]);
                     __syncwarp();
-                    eq.next(L::kQStages);
+                    eq.next(q_stages);
                 }
             }
             if (!ok) break;
             if (ptx::elect_one()) ptx::umma_commit(&bars->k_empty[ek.stage]);
             __syncwarp();
-            ek.next(L::kPairs);
+            ek.next(k_stages);
         }
     } else {
         // ================= Softmax warps: two threads per key, 64 columns of a tile each =================
@@ -311,36 +316,48 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         const int from = max(key - seg.seen0 + 1 - first, 0) * shape.group - half * kHalf, to = columns - half * kHalf;
                         const bool masked = columns < kTile || (kt + u) * kTile + kTile - 1 - seg.seen0 + 1 > first;
                         const float4* nlse = reinterpret_cast<const float4*>(smem + L::kLseOff + eq.stage * kTile * 4) + half * (kHalf / 4);
-#pragma unroll 1
-                        for (int c = 0; c < kHalf && c < to; c += kChunk) {
-                            uint32_t s[kChunk];
-                            ptx::tmem_ld_32x32b_x32(t_own + static_cast<uint32_t>(buffer * kTile + c), s);
+                        if (to > 0) {  // (the columns of few rows lie in the first half)
+                            // all scores to registers: the buffer goes back, and the exponentials have nothing to wait for
+                            uint32_t s0[kChunk], s1[kChunk];
+                            ptx::tmem_ld_32x32b_x32(t_own + static_cast<uint32_t>(buffer * kTile), s0);
+                            ptx::tmem_ld_32x32b_x32(t_own + static_cast<uint32_t>(buffer * kTile + kChunk), s1);
                             ptx::tmem_wait_ld();
+                            ptx::tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(&bars->s_free[u][buffer]);
+                            auto add_up = [&](const uint32_t(&s)[kChunk], int c, auto some) {
 #pragma unroll
-                            for (int i = 0; i < kChunk; i += 4) {
-                                const float4 n = nlse[(c + i) / 4];
-                                float x[4];
-                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2c2, ptx::pack2(n.x, n.y)), x[0], x[1]);
-                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2c2, ptx::pack2(n.z, n.w)), x[2], x[3]);
+                                for (int i = 0; i < kChunk; i += 4) {
+                                    const float4 n = nlse[(c + i) / 4];
+                                    float x[4];
+                                    ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2c2, ptx::pack2(n.x, n.y)), x[0], x[1]);
+                                    ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2c2, ptx::pack2(n.z, n.w)), x[2], x[3]);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) x[e] = ptx::ex2_approx(x[e]);
-                                if (masked) {
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) x[e] = c + i + e >= from && c + i + e < to ? x[e] : 0.0f;
+                                    for (int e = 0; e < 4; ++e) {
+                                        x[e] = ptx::ex2_approx(x[e]);
+                                        if constexpr (decltype(some)::value) x[e] = c + i + e >= from && c + i + e < to ? x[e] : 0.0f;
+                                    }
+                                    acc[(i >> 1) & 3] = ptx::add2(acc[(i >> 1) & 3], ptx::pack2(x[0], x[1]));
+                                    acc[((i >> 1) + 1) & 3] = ptx::add2(acc[((i >> 1) + 1) & 3], ptx::pack2(x[2], x[3]));
                                 }
-                                acc[(i >> 1) & 3] = ptx::add2(acc[(i >> 1) & 3], ptx::pack2(x[0], x[1]));
-                                acc[((i >> 1) + 1) & 3] = ptx::add2(acc[((i >> 1) + 1) & 3], ptx::pack2(x[2], x[3]));
+                            };
+                            if (masked) {
+                                add_up(s0, 0, std::true_type{});
+                                if (to > kChunk) add_up(s1, kChunk, std::true_type{});
+                            } else {
+                                add_up(s0, 0, std::false_type{});
+                                add_up(s1, kChunk, std::false_type{});
                             }
+                        } else {
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(&bars->s_free[u][buffer]);
                         }
-                        ptx::tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive(&bars->s_free[u][buffer]);
                     }
                 }
                 if (!resident) {
                     __syncwarp();
                     if (ok && lane == 0) ptx::mbar_arrive(&bars->q_empty[eq.stage]);
-                    eq.next(L::kQStages);
+                    eq.next(q_stages);
                 }
             }
             // the halves of a key's columns meet in shared memory (even and odd pairs in places of their own: nobody is two pairs ahead)
@@ -370,8 +387,8 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     while (!ptx::mbar_try_wait(&full[it % stages], static_cast<uint32_t>(it / stages) & 1u) && clock64() - t0 < kWaitLimitCycles / 8) {
                     }
             };
-            land(bars->k_full, L::kPairs, k_loads);
-            land(bars->q_full, L::kQStages, q_loads);
+            land(bars->k_full, k_stages, k_loads);
+            land(bars->q_full, q_stages, q_loads);
         }
     }
     if (warp == kMma) {
