@@ -1,10 +1,11 @@
 // Eviction from a paged cache by accumulated attention weight: of a sequence that is longer than its budget, each key head keeps the
 // latest `recent` keys and, of the others, those of most weight; they move together, in their order.
 //
-// evict_select: one CTA a row (sequence, key head).  The weights become integers of the same order; three passes of 11 bits find the
-// smallest one that stays (a radix select: 11 bits, because the weights of a cache share their exponents' upper bits and a histogram of
-// them would be one long queue of atomics at a few addresses), a fourth pass numbers the keys that stay.  Of equal weights at the
-// border the lowest indices stay.  The passes read the row again, out of L2: three quarters of a microsecond each at 16384 keys.
+// evict_select: one CTA a row (sequence, key head).  The weights become integers of the same order; a histogram of their upper 13 bits (sign, exponent
+// and four digits: the weights of a cache share their exponents' upper bits, and few bins would be a queue of atomics at each) tells which stay, but for
+// those of one bin, of which the largest have room.  If that bin has at most kList weights, each counts those in front of it; if not, another 11 and 8
+// bits, and of weights that are equal to the last bit the first ones stay.  Who stays is a bit a key in shared memory; a sum over the words' bits gives
+// the new places.  Up to 16384 keys are read once, into registers; longer rows in turns of as many, again for each step (out of L2).
 //
 // evict_move: to pages of their own, any CTA takes any keys.  In place, key t comes from index kept[t] >= t, so a row can be moved in
 // ascending steps - all of a step read before any of it is written - and nothing is overwritten that a later step reads.  The steps of
@@ -19,22 +20,28 @@ namespace attnw {
 namespace evict {
 
 constexpr int kSelectThreads = 1024;
-constexpr int kBins = 2048;
+constexpr int kBins = 8192, kBinsEach = kBins / kSelectThreads;
+constexpr int kHeld = 16;                             // weights that a thread holds
+constexpr int kRound = kSelectThreads * kHeld;        // keys of a turn
+constexpr int kList = 1024;
 
 // Larger weight, larger integer; both zeros alike; a NaN is below every number.
 __device__ __forceinline__ uint32_t order_of(float x) {
-    if (x != x) return 0u;
-    const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(x + 0.0f);  // (-0 + 0 is +0)
+    const uint32_t k = u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);
+    return x == x ? k : 0u;
 }
 
 struct SelectSmem {
     uint32_t bins[kBins];
     uint32_t warp_sum[32];
-    uint32_t digit, above;  // the chosen bin and the keys above it
+    uint32_t digit, above, in_bin;  // the chosen bin, the keys above it, and in it
+    uint32_t listed;
+    unsigned long long list[kList];  // weight's integer << 32 | ~index: the larger, the earlier
+    // then dynamic: words of bits, [turns' words] and the sums in front of them
 };
 
-// Inclusive sum over the block's threads; `total` to all.  One use between two __syncthreads of the caller's.
+// Inclusive sum over the block's threads; `total` to all.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* warp_sum, uint32_t* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -60,12 +67,30 @@ __global__ void __launch_bounds__(kSelectThreads)
 evict_select_kernel(paged::Cache cache, const float* mass, float* mass_out, int* kept, int* lengths_out, int budget, int recent, int capacity,
                     int capacity_out) {
     __shared__ SelectSmem sm;
-    const int tid = static_cast<int>(threadIdx.x);
+    __shared__ uint32_t words[kRound / 32], equals[kRound / 32], before[kRound / 32];  // of a turn
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
     const int b = static_cast<int>(blockIdx.x) / cache.kv_heads;
     ptx::grid_dependency_wait();
     const float* row = mass + static_cast<size_t>(blockIdx.x) * capacity;
     float* out = mass_out + static_cast<size_t>(blockIdx.x) * capacity_out;
     int* keep = kept + static_cast<size_t>(blockIdx.x) * budget;
+    // This thread's weights of a turn, as integers: word (e * 32 + warp) of the turn's, bit `lane`.
+    uint32_t key[kHeld];
+    auto index_of = [&](int turn0, int e) { return turn0 + (e * 32 + warp) * 32 + lane; };
+    auto values = [&](int turn0, int end, float (&x)[kHeld]) {  // (all loads, then what is made of them: one latency)
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) {
+            const int i = index_of(turn0, e);
+            x[e] = i < end ? row[i] : 0.0f;
+        }
+    };
+    auto load = [&](int turn0, int end) {
+        float x[kHeld];
+        values(turn0, end, x);
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e) key[e] = order_of(x[e]);
+    };
+    load(0, capacity);  // (beside the length)
     const int length = paged::length_of(cache, b);
     const int left = min(length, budget);
     if (tid == 0 && blockIdx.x % cache.kv_heads == 0) lengths_out[b] = left;
@@ -73,83 +98,154 @@ evict_select_kernel(paged::Cache cache, const float* mass, float* mass_out, int*
     const int chosen = length > budget ? budget - recent : 0;
 
     if (chosen > 0) {
-        uint32_t prefix = 0, mask = 0, need = static_cast<uint32_t>(chosen);
-        constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
-#pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = kShift[pass], bins = 1 << kBits[pass];
-            for (int i = tid; i < kBins; i += kSelectThreads) sm.bins[i] = 0;
-            __syncthreads();
-            for (int i0 = 0; i0 < old; i0 += kSelectThreads) {
-                const int i = i0 + tid;
-                const uint32_t key = i < old ? order_of(row[i]) : 0u;
-                const bool in = i < old && (key & mask) == prefix;
-                const uint32_t bin = (key >> shift) & static_cast<uint32_t>(bins - 1);
-                // (a row of equal weights would be one queue: a warp of equals adds once)
-                int same;
-                __match_all_sync(0xffffffffu, in ? bin : 0xffffffffu, &same);
-                if (same) {
-                    if (in && (tid & 31) == 0) atomicAdd(&sm.bins[bin], 32u);
-                } else if (in) {
-                    atomicAdd(&sm.bins[bin], 1u);
+        const bool once = old <= kRound;
+        for (int i = tid; i < kBins; i += kSelectThreads) sm.bins[i] = 0;
+        if (tid == 0) sm.listed = 0;
+        __syncthreads();
+        // ---- the smallest weight that stays, as far as needed: all bits of `mask` ----
+        uint32_t prefix = 0, mask = 0, need = static_cast<uint32_t>(chosen), shift = 19, bits = 13;
+        for (;;) {
+            for (int turn0 = 0; turn0 < old; turn0 += kRound) {
+                if (!once) load(turn0, old);
+#pragma unroll
+                for (int e = 0; e < kHeld; ++e) {
+                    const int i = index_of(turn0, e);
+                    if (i - lane >= old) break;  // (the whole warp)
+                    if (i < old && (key[e] & mask) == prefix) atomicAdd(&sm.bins[(key[e] >> shift) & ((1u << bits) - 1u)], 1u);
                 }
             }
             __syncthreads();
             // from the largest bin down: the one in which the sum reaches `need`
-            const int hi = bins - 1 - 2 * tid;  // this thread's bins hi and hi - 1
-            const uint32_t c0 = hi >= 1 ? sm.bins[hi] : 0u, c1 = hi >= 1 ? sm.bins[hi - 1] : 0u;
-            uint32_t total;
-            const uint32_t upto = block_scan(c0 + c1, sm.warp_sum, &total), before = upto - c0 - c1;
-            if (before < need && need <= upto) {
-                const bool first = need <= before + c0;
-                sm.digit = static_cast<uint32_t>(first ? hi : hi - 1);
-                sm.above = first ? before : before + c0;
+            const int hi = (1 << bits) - 1 - kBinsEach * tid;  // this thread's bins hi ... hi - kBinsEach + 1
+            uint32_t c[kBinsEach], own = 0;
+#pragma unroll
+            for (int k = 0; k < kBinsEach; ++k) {
+                c[k] = hi - k >= 0 ? sm.bins[hi - k] : 0u;
+                own += c[k];
+            }
+            uint32_t total, in_front = block_scan(own, sm.warp_sum, &total) - own;
+            if (in_front < need && need <= in_front + own) {
+#pragma unroll
+                for (int k = 0; k < kBinsEach; ++k) {
+                    if (in_front < need && need <= in_front + c[k]) {
+                        sm.digit = static_cast<uint32_t>(hi - k);
+                        sm.above = in_front;
+                        sm.in_bin = c[k];
+                    }
+                    in_front += c[k];
+                }
             }
             __syncthreads();
             prefix |= sm.digit << shift;
-            mask |= static_cast<uint32_t>(bins - 1) << shift;
+            mask |= ((1u << bits) - 1u) << shift;
             need -= sm.above;
+            if (sm.in_bin <= kList || shift == 0) break;
+            bits = shift == 19 ? 11 : 8;
+            shift = shift == 19 ? 8 : 0;
+            for (int i = tid; i < kBins; i += kSelectThreads) sm.bins[i] = 0;
+            __syncthreads();
         }
-        // `prefix` is the smallest weight that stays; of those equal to it the first `need`.
-        uint32_t done_above = 0, done_equal = 0;
-        for (int i0 = 0; i0 < old; i0 += 4 * kSelectThreads) {
-            float x[4];
-            uint32_t counts = 0;  // above in the low half, equal in the high half
+        // Of those with the prefix the first `need` stay, by weight, then by index: all weights above `border`, and those equal to it up to index
+        // `last` (by_list) or the first `need` (then mask has all bits).
+        const bool by_list = sm.in_bin <= kList;
+        uint32_t border = prefix;
+        int last = -1;
+        if (by_list) {
+            for (int turn0 = 0; turn0 < old; turn0 += kRound) {
+                if (!once) load(turn0, old);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = i0 + 4 * tid + e;
-                x[e] = i < old ? row[i] : 0.0f;
-                const uint32_t key = i < old ? order_of(x[e]) : 0u;
-                counts += i < old && key > prefix ? 1u : i < old && key == prefix ? 0x10000u : 0u;
-            }
-            uint32_t total;
-            const uint32_t before = block_scan(counts, sm.warp_sum, &total) - counts;  // (its barriers: all have read before any writes)
-            uint32_t above = done_above + (before & 0xffffu), equal = done_equal + (before >> 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = i0 + 4 * tid + e;
-                if (i >= old) break;
-                const uint32_t key = order_of(x[e]);
-                if (key > prefix || (key == prefix && equal < need)) {
-                    const uint32_t at = above + min(equal, need);
-                    keep[at] = i;
-                    out[at] = x[e];
+                for (int e = 0; e < kHeld; ++e) {
+                    const int i = index_of(turn0, e);
+                    if (i - lane >= old) break;
+                    if (i < old && (key[e] & mask) == prefix)
+                        sm.list[atomicAdd(&sm.listed, 1u)] = static_cast<unsigned long long>(key[e]) << 32 | static_cast<uint32_t>(~i);
                 }
-                above += key > prefix ? 1u : 0u;
-                equal += key == prefix ? 1u : 0u;
             }
-            done_above += total & 0xffffu;
-            done_equal += total >> 16;
+            __syncthreads();
+            const int n = static_cast<int>(sm.listed);
+            if (tid < n) {
+                const unsigned long long mine = sm.list[tid];
+                uint32_t in_front = 0;
+#pragma unroll 8
+                for (int i = 0; i < n; ++i) in_front += sm.list[i] > mine ? 1u : 0u;
+                if (in_front + 1u == need) {  // one of them
+                    sm.digit = static_cast<uint32_t>(mine >> 32);
+                    sm.above = ~static_cast<uint32_t>(mine);
+                }
+            }
+            __syncthreads();
+            border = sm.digit;
+            last = static_cast<int>(sm.above);
+        }
+        // ---- the new places ----
+        uint32_t done = 0, done_equal = 0;
+        for (int turn0 = 0; turn0 < old; turn0 += kRound) {
+            if (!once) load(turn0, old);
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e) {
+                const int i = index_of(turn0, e);
+                if (i - lane >= old) break;
+                const bool equal = i < old && key[e] == border;
+                const uint32_t word = __ballot_sync(0xffffffffu, i < old && (key[e] > border || (equal && i <= last)));
+                const uint32_t same = by_list ? 0u : __ballot_sync(0xffffffffu, equal);
+                if (lane == 0) {
+                    words[e * 32 + warp] = word;
+                    equals[e * 32 + warp] = same;
+                }
+            }
+            __syncthreads();
+            static_assert(kRound / 32 <= kSelectThreads, "a thread a word");
+            const bool has_word = tid < kRound / 32 && turn0 + tid * 32 < old;
+            uint32_t word = has_word ? words[tid] : 0u, total;
+            if (!by_list) {  // the first `need` of the equal ones
+                const uint32_t same = has_word ? equals[tid] : 0u, count = static_cast<uint32_t>(__popc(same));
+                const uint32_t in_front = done_equal + block_scan(count, sm.warp_sum, &total) - count;
+                uint32_t some = same;
+                if (in_front + count > need) {
+                    some = 0;
+                    for (uint32_t k = in_front, rest = same; k < need; ++k) {
+                        some |= rest & (0u - rest);
+                        rest &= rest - 1u;
+                    }
+                }
+                word |= some;
+                if (has_word) words[tid] = word;
+                done_equal += total;
+            }
+            const uint32_t count = static_cast<uint32_t>(__popc(word));
+            const uint32_t in_front = done + block_scan(count, sm.warp_sum, &total) - count;
+            if (has_word) before[tid] = in_front;
+            done += total;
+            // the weights themselves, where their integers do not tell (zeros, NaN), before any is written
+            float odd[kHeld];
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e) {
+                const int i = index_of(turn0, e);
+                odd[e] = i < old && (key[e] == 0u || key[e] == 0x80000000u) ? row[i] : 0.0f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e) {
+                const int i = index_of(turn0, e);
+                if (i - lane >= old) break;
+                const uint32_t w = words[e * 32 + warp];
+                if (w >> lane & 1u) {
+                    const uint32_t at = before[e * 32 + warp] + static_cast<uint32_t>(__popc(w & ((1u << lane) - 1u)));
+                    keep[at] = i;
+                    out[at] = key[e] == 0u || key[e] == 0x80000000u ? odd[e] : __uint_as_float(key[e] & 0x80000000u ? key[e] ^ 0x80000000u : ~key[e]);
+                }
+            }
+            __syncthreads();
         }
     }
     // the keys that stay anyway; nothing behind them
     for (int t0 = chosen; t0 < left; t0 += kSelectThreads) {
         const int t = t0 + tid;
-        const float x = t < left ? row[old + t - chosen] : 0.0f;
+        const float v = t < left ? row[old + t - chosen] : 0.0f;
         __syncthreads();
         if (t < left) {
             keep[t] = old + t - chosen;
-            out[t] = x;
+            out[t] = v;
         }
         __syncthreads();
     }
