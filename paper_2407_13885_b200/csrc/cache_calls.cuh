@@ -63,9 +63,9 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 // Heads that one thread walks with its cosines and sines: all of them where the tokens alone fill the device (1024 threads an SM), fewer
 // otherwise, since latency is what a small call spends its time on.
-int heads_each(long long threads, int heads, int sm_count) {
+int heads_each(long long threads, int heads, int sm_count, int most) {
     const long long groups = std::max(1ll, static_cast<long long>(sm_count) * 1024 / std::max(1ll, threads));
-    return static_cast<int>((heads + groups - 1) / groups);
+    return static_cast<int>(std::min(static_cast<long long>(most), (heads + groups - 1) / groups));
 }
 
 template <typename T>
@@ -95,7 +95,7 @@ int rope_entry(const void* X, const int* positions, const double* frequencies, v
     const int parts = d / (2 * rope::Vec<T>::kN);
     const long long threads = static_cast<long long>(tokens) * parts, blocks = (threads + rope::kThreads - 1) / rope::kThreads;
     if (blocks > INT_MAX) return ATTNW_ERR_BAD_SHAPE;
-    const int each = heads_each(threads, H, dev->sm_count);
+    const int each = heads_each(threads, H, dev->sm_count, 8);
     const rope::Rows rows{X, Y, x_strides[0], x_strides[2], x_strides[1], y_strides[0], y_strides[2], y_strides[1], H};
     const rope::Turn turn{positions, frequencies, rotary, amplitude, inverse ? -1.0f : 1.0f};
     const auto kernel = layout == 0 ? rope::rope_kernel<T, true> : rope::rope_kernel<T, false>;
@@ -178,7 +178,7 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
     if (rc != ATTNW_OK) return rc;
     const int parts = c->d / 16;
     const long long threads = static_cast<long long>(tokens) * parts, blocks = (threads + rope::kThreads - 1) / rope::kThreads;
-    const int rows = (Q ? heads : 0) + 2 * c->kv_heads, each = std::min(heads_each(threads, rows, dev->sm_count), std::max(Q ? heads : 1, c->kv_heads));
+    const int rows = (Q ? heads : 0) + 2 * c->kv_heads, each = std::min(heads_each(threads, rows, dev->sm_count, 16), std::max(Q ? heads : 1, c->kv_heads));
     const int q_groups = Q ? (heads + each - 1) / each : 0, kv_groups = (c->kv_heads + each - 1) / each;
     if (q_groups + 2 * kv_groups > 65535) return ATTNW_ERR_BAD_SHAPE;
     const rope::Rows q{Q, Q_out, 0, strides[0], strides[1], 0, strides[6], strides[7], heads}, k_rows{K, nullptr, 0, strides[2], strides[3], 0, 0, 0, c->kv_heads},

@@ -113,12 +113,13 @@ struct Lane {
     }
 };
 
-// Rows of one token, heads h0 ... h1 - 1, four at a time in flight.
-template <typename T, bool HALF, bool TURN>
-__device__ __forceinline__ void walk(const Lane<T, HALF>& lane, const T* src, long long src_head, T* dst, long long dst_head, int count) {
-    constexpr int kFlight = 4;
-    for (int h = 0; h < count; h += kFlight) {
-        uint4 v0[kFlight], v1[kFlight];
+// Rows of one token, `count` heads, kFlight of them on their way at a time.
+constexpr int kFlight = 4;
+
+template <typename T, bool HALF>
+struct Rows4 {
+    uint4 v0[kFlight], v1[kFlight];
+    __device__ __forceinline__ void load(const Lane<T, HALF>& lane, const T* src, long long src_head, int h, int count) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
             if (h + i < count) {
@@ -126,6 +127,9 @@ __device__ __forceinline__ void walk(const Lane<T, HALF>& lane, const T* src, lo
                 v0[i] = __ldcs(reinterpret_cast<const uint4*>(row + lane.off0));
                 v1[i] = __ldcs(reinterpret_cast<const uint4*>(row + lane.off1));
             }
+    }
+    template <bool TURN>
+    __device__ __forceinline__ void store(const Lane<T, HALF>& lane, T* dst, long long dst_head, int h, int count) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
             if (h + i < count) {
@@ -134,6 +138,17 @@ __device__ __forceinline__ void walk(const Lane<T, HALF>& lane, const T* src, lo
                 *reinterpret_cast<uint4*>(row + lane.off0) = v0[i];
                 *reinterpret_cast<uint4*>(row + lane.off1) = v1[i];
             }
+    }
+};
+
+// The first rows have been loaded.
+template <typename T, bool HALF, bool TURN>
+__device__ __forceinline__ void walk(const Lane<T, HALF>& lane, Rows4<T, HALF>& rows, const T* src, long long src_head, T* dst, long long dst_head, int count) {
+    for (int h = 0;;) {
+        rows.template store<TURN>(lane, dst, dst_head, h, count);
+        h += kFlight;
+        if (h >= count) break;
+        rows.load(lane, src, src_head, h, count);
     }
 }
 
@@ -147,12 +162,14 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(Rows rows, Turn turn, lo
     if (token >= tokens) return;
     Lane<T, HALF> lane;
     lane.place(part, turn.rotary);
-    lane.angles(turn, part, token);
-    const int h0 = static_cast<int>(blockIdx.y) * heads_each;
+    const int h0 = static_cast<int>(blockIdx.y) * heads_each, count = min(heads_each, rows.heads - h0);
     const long long b = token / per_batch, n = token % per_batch;
-    walk<T, HALF, true>(lane, static_cast<const T*>(rows.src) + b * rows.src_batch + n * rows.src_token + h0 * rows.src_head, rows.src_head,
-                        static_cast<T*>(rows.dst) + b * rows.dst_batch + n * rows.dst_token + h0 * rows.dst_head, rows.dst_head,
-                        min(heads_each, rows.heads - h0));
+    const T* src = static_cast<const T*>(rows.src) + b * rows.src_batch + n * rows.src_token + h0 * rows.src_head;
+    Rows4<T, HALF> held;
+    held.load(lane, src, rows.src_head, 0, count);
+    lane.angles(turn, part, token);
+    walk<T, HALF, true>(lane, held, src, rows.src_head, static_cast<T*>(rows.dst) + b * rows.dst_batch + n * rows.dst_token + h0 * rows.dst_head, rows.dst_head,
+                        count);
 }
 
 // Grid: x over (token, part); y over groups of heads, those of the queries first, then those of the keys, then the values'.
@@ -162,21 +179,26 @@ append_kernel(Rows q, Rows k, Rows v, paged::Cache cache, const int* starts, Tur
     using T = __nv_bfloat16;
     __shared__ paged::Samples samples;
     ptx::grid_dependency_wait();
-    paged::sample_starts(&samples, starts, cache.sequences, kThreads);
-    __syncthreads();
     const long long id = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
     const long long token = id / parts;
     const int part = static_cast<int>(id % parts);
-    if (token >= tokens) return;
-    int end;
-    const int b = paged::owner_of(&samples, starts, cache.sequences, static_cast<int>(token), &end);
-    if (b < 0) return;
     int group = static_cast<int>(blockIdx.y);
     const int kind = group < q_groups ? 0 : group < q_groups + kv_groups ? 1 : 2;
     group -= kind == 0 ? 0 : kind == 1 ? q_groups : q_groups + kv_groups;
     const Rows& rows = kind == 0 ? q : kind == 1 ? k : v;
     const int h0 = group * heads_each, count = min(heads_each, rows.heads - h0);
     const T* src = static_cast<const T*>(rows.src) + token * rows.src_token + h0 * rows.src_head;
+    Lane<T, HALF> lane;
+    lane.place(part, turn.rotary);
+    // (the rows are on their way while the token's sequence and place are looked up)
+    Rows4<T, HALF> held;
+    if (token < tokens) held.load(lane, src, rows.src_head, 0, count);
+    paged::sample_starts(&samples, starts, cache.sequences, kThreads);
+    __syncthreads();
+    if (token >= tokens) return;
+    int end;
+    const int b = paged::owner_of(&samples, starts, cache.sequences, static_cast<int>(token), &end);
+    if (b < 0) return;
     T* dst;
     long long dst_head;
     if (kind == 0) {
@@ -190,13 +212,11 @@ append_kernel(Rows q, Rows k, Rows v, paged::Cache cache, const int* starts, Tur
         dst = (kind == 1 ? cache.K : cache.V) + paged::row_offset(cache, page, h0, at);
         dst_head = static_cast<long long>(cache.d) << cache.page_shift;
     }
-    Lane<T, HALF> lane;
-    lane.place(part, turn.rotary);
     if (kind != 2 && turn.positions) {
         lane.angles(turn, part, token);
-        walk<T, HALF, true>(lane, src, rows.src_head, dst, dst_head, count);
+        walk<T, HALF, true>(lane, held, src, rows.src_head, dst, dst_head, count);
     } else {
-        walk<T, HALF, false>(lane, src, rows.src_head, dst, dst_head, count);
+        walk<T, HALF, false>(lane, held, src, rows.src_head, dst, dst_head, count);
     }
 }
 
