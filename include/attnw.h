@@ -9,10 +9,12 @@
  *                  Grayskull"; the product is Attention's softmax(QK^T/sqrt(d_k)) of Section IV).
  *   softmax_rows*  row-wise Softmax of precomputed scores (the dedicated kernel of
  *                  Section VI-B; definition in Section VI, max subtraction of Eq. 1).
+ *   attnw_rope*, attnw_cache_append, attn_paged, attnw_cache_evict  generating token by token: rotary positions, a paged cache of keys and
+ *                  values, Attention of new tokens over it, and its shortening by the attention weights that its keys have received.
  *
  * Conventions shared by the device entry points
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library neither
- *     allocates nor frees device memory in these calls.  Tensors are row-major and contiguous.
+ *     allocates nor frees device memory in these calls.  Tensors are row-major and contiguous where no strides are given.
  *   - `stream` is a cudaStream_t (NULL = the legacy default stream).  Calls enqueue work and
  *     return; they do not synchronise.
  *   - The return value is an attnw_status.  Argument errors are detected on the host and
@@ -35,7 +37,7 @@ typedef enum attnw_status {
     ATTNW_ERR_NULL_POINTER = 1, /* a required pointer is NULL                                   */
     ATTNW_ERR_BAD_SHAPE = 2,    /* a size is < 1, overflows, or scale is negative / not finite  */
     ATTNW_ERR_MISALIGNED = 3,   /* pointer not 16-byte aligned, or row pitch not 16-byte sized  */
-    ATTNW_ERR_UNSUPPORTED = 4,  /* d not in {64, 128}; device is not sm_100                     */
+    ATTNW_ERR_UNSUPPORTED = 4,  /* d not in {64, 128}, another size a call names; device is not sm_100 */
     ATTNW_ERR_CUDA = 5,         /* a CUDA runtime / driver call failed (launch, map encode)     */
     ATTNW_ERR_TIMEOUT = 6,      /* a bounded device-side wait gave up (see attnw_query_status)  */
     ATTNW_ERR_ALIASING = 7      /* output overlaps an input in a way the kernel cannot allow    */
@@ -319,7 +321,7 @@ int attnw_host_release(void);
  * up records a code in a per-device status word, makes the kernel unwind and return normally, and the output of
  * that launch is then undefined.
  * The word is STICKY: while it is non-zero, every later launch of the tensor-core kernels (attnw_fused*, attn_fused,
- * attnw_project_qk) and of the shared-memory and cluster tiers of softmax_rows* (rows of 8193 to 262144 columns, but
+ * attnw_project_qk, attn_paged but for its kernel for few tokens) and of the shared-memory and cluster tiers of softmax_rows* (rows of 8193 to 262144 columns, but
  * for those that are read twice) ends after its set-up and first loads WITHOUT WRITING ITS OUTPUT - the
  * call itself still returns ATTNW_OK, since it only enqueues - so that no work piles up behind a device that has
  * stopped making progress.  The register and streaming tiers of softmax_rows* have no waits and ignore the word.

@@ -1203,7 +1203,7 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
 }
 
 long long attn_paged_workspace(const attnw_cache* cache, int tokens, int heads, int weigh) {
-    if (!cache || tokens < 1 || heads < 1 || cache->kv_heads < 1 || heads % cache->kv_heads != 0 || heads / cache->kv_heads > 128) return 0;
+    if (check_cache(cache) != ATTNW_OK || tokens < 1 || heads < 1 || heads % cache->kv_heads != 0 || heads / cache->kv_heads > 128) return 0;
     return static_cast<long long>(paged_workspace(cache, tokens, heads, weigh != 0).bytes);
 }
 
@@ -1437,7 +1437,7 @@ const char* attnw_strerror(int code) {
         case ATTNW_ERR_NULL_POINTER: return "a required pointer is NULL";
         case ATTNW_ERR_BAD_SHAPE: return "a size is out of range, or scale is negative or not finite";
         case ATTNW_ERR_MISALIGNED: return "a pointer or a row pitch is not a multiple of 16 bytes";
-        case ATTNW_ERR_UNSUPPORTED: return "unsupported head dimension or device (needs d in {64,128}, sm_100)";
+        case ATTNW_ERR_UNSUPPORTED: return "unsupported head dimension (needs d in {64,128}), size or device (needs sm_100)";
         case ATTNW_ERR_CUDA: return "a CUDA runtime or driver call failed";
         case ATTNW_ERR_TIMEOUT: return "a bounded device-side wait gave up; the output of that launch is undefined";
         case ATTNW_ERR_ALIASING: return "the output overlaps an input";

@@ -17,7 +17,7 @@ struct Extent {
 int check_strides(const long long* strides, const long long* sizes, int n, int esize, bool written) {
     for (int i = 0; i < n; ++i) {
         if (sizes[i] <= 1) continue;
-        if (strides[i] < 0 || strides[i] > (1ll << 40)) return ATTNW_ERR_BAD_SHAPE;
+        if (strides[i] < 0 || strides[i] > (1ll << 47) / (sizes[i] - 1)) return ATTNW_ERR_BAD_SHAPE;  // (an array lies within 2^48 elements)
         if (strides[i] * esize % 16 != 0) return ATTNW_ERR_MISALIGNED;
         if (written && strides[i] == 0) return ATTNW_ERR_BAD_SHAPE;
     }
@@ -351,8 +351,9 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     if (heads / c->kv_heads > 128) return ATTNW_ERR_UNSUPPORTED;
     if (static_cast<long long>(tokens) * heads > INT_MAX / 4) return ATTNW_ERR_BAD_SHAPE;
     const long long sizes[2] = {tokens, heads};
-    rc = check_strides(q_strides, sizes, 2, 2, true);  // (a tensor map has no broadcast dimensions)
+    rc = check_strides(q_strides, sizes, 2, 2, true);  // (a tensor map has no broadcast dimensions, and strides below 2^40 bytes)
     if (rc != ATTNW_OK) return rc;
+    if ((tokens > 1 && q_strides[0] >= 1ll << 39) || (heads > 1 && q_strides[1] * (heads / c->kv_heads) >= 1ll << 39)) return ATTNW_ERR_BAD_SHAPE;
     if (!aligned16(Q) || !aligned16(O) || !aligned4(starts) || !aligned4(lse) || !aligned4(mass) || !aligned4(mass_out)) return ATTNW_ERR_MISALIGNED;
     const unsigned long long capacity = static_cast<unsigned long long>(c->table_width) * c->page, weights = 4ull * c->sequences * c->kv_heads * capacity;
     const PagedWorkspace w = paged_workspace(c, tokens, heads, mass != nullptr);

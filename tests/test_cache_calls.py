@@ -116,6 +116,7 @@ def test_attention_argument_errors(binding):
     assert f(mass=0xa000000, mass_out=0xa000000 + 64) == 7 and f(mass=Y, mass_out=0xa000000) == 7 and f(mass=0xa000000, mass_out=Y) == 7
     assert f(mass=0xa000000, mass_out=0xa000000, w=Y) == 7
     assert f(tokens=1 << 29, heads=2, s=(128, 64)) == 2
+    assert f(s=(1 << 39, 64)) == 2 and f(s=(1 << 62, 64)) == 2 and f(s=(256, 1 << 38)) == 2
 
 
 def test_evict_argument_errors(binding):
@@ -139,7 +140,13 @@ def test_paged_variant_knob(binding):
 
 def test_workspace_needs_a_cache(binding):
     assert binding.lib.attn_paged_workspace(None, 4, 4, 1) == 0
-    assert binding.lib.attn_paged_workspace(cache(binding), 0, 4, 1) == 0
+    assert binding.lib.attn_paged_workspace(cache(binding), 0, 4, 1) == 0 and binding.lib.attn_paged_workspace(cache(binding), 4, 5, 1) == 0
+    for changes, _ in BAD_CACHES:
+        assert binding.lib.attn_paged_workspace(cache(binding, **changes), 4, 4, 1) == 0
+    assert binding.lib.attn_paged_workspace(cache(binding), 4, 4, 1) > 0
+    # a longer table may need more, never less
+    sizes = [binding.lib.attn_paged_workspace(cache(binding, table_width=w), 40, 4, 0) for w in (1, 8, 63, 64, 1000)]
+    assert sizes == sorted(sizes) and sizes[0] == 0
 
 
 def test_host_tensors_and_shapes_are_refused(binding):

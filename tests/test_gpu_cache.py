@@ -238,6 +238,13 @@ ATTENTION = [
     (16, 8, 64, 64, [(1, 9000 + 100 * i) for i in range(8)]),
     (8, 1, 128, 128, [(300, 8500)]),
     (32, 8, 64, 32, [(300, 5000), (33, 5100)]),
+    # more sequences than a warp has lanes, some without new tokens or without keys
+    (4, 2, 64, 16, [(i % 3, (37 * i) % 400) for i in range(110)]),
+    (2, 1, 128, 32, [(0, 50)] * 40 + [(1, 900)] + [(0, 0)] * 40 + [(70, 1500)]),
+    # clusters of 7, 5 and 3 CTAs where few tokens are served by clusters
+    (6, 3, 64, 16, [(1, 700 + i) for i in range(7)]),
+    (5, 5, 128, 16, [(1, 900 - 33 * i) for i in range(5)]),
+    (16, 16, 64, 16, [(1, 300), (1, 17), (1, 0)]),
 ]
 
 
@@ -276,6 +283,157 @@ def test_attention_with_bad_pages_lengths_and_starts(attnw, variant):
                          mass=torch.zeros(2, 2, 80, device="cuda"))
     torch.cuda.synchronize()
     assert attnw.query_status() == 0
+
+
+def test_attention_over_shared_pages_is_the_same_for_both(attnw, variant):
+    # two sequences whose tables name the same pages: a prompt that both begin with
+    c = Paged([(1, 300), (1, 300)], 2, 64, 16, seed=2)
+    c.table[1] = c.table[0]
+    Q = c.normal(2, 8, 64)
+    Q[1] = Q[0]
+    O, lse, mass = check_attention(attnw, c, Q, 0.125)
+    assert torch.equal(O[0], O[1]) and torch.equal(lse[0], lse[1])
+
+
+def test_caches_beyond_two_and_four_gigabytes(attnw, variant):
+    # places whose offsets pass 2^31 elements and 2^32 bytes
+    pages, Hkv, page, d = 40000, 8, 64, 128
+    K, V = (torch.empty(pages, Hkv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = Paged([(3, 130), (1, 64)], Hkv, d, page, seed=4)
+    ids = torch.tensor([[39999, 33000, 7], [39998, 0, 0]], dtype=torch.int32, device="cuda")
+    for b in range(2):
+        for i in range(-(-c.pairs[b][1] // page)):
+            K[int(ids[b, i])], V[int(ids[b, i])] = c.K[int(c.table[b, i])], c.V[int(c.table[b, i])]
+    Q = c.normal(4, 16, d)
+    mass = torch.zeros(2, Hkv, 3 * page, device="cuda")
+    want = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, 0.09, mass=mass)
+    got = attnw.attn_paged(Q, K, V, ids, c.lengths, c.starts, 0.09, mass=mass)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    k, v = c.normal(4, Hkv, d), c.normal(4, Hkv, d)
+    attnw.cache_append(None, k, v, K, V, ids, c.lengths, c.starts)
+    assert torch.equal(K[7, :, 0:2], k[1:3].transpose(0, 1)) and torch.equal(V[39998, :, 63], v[3]) and torch.equal(K[33000, :, 63], k[0])
+    out = torch.tensor([[38000], [38001]], dtype=torch.int32, device="cuda")
+    kept, _, _ = attnw.cache_evict(K, V, ids, c.lengths, want[1], 40, 4, table_out=out)
+    for b in range(2):
+        src = kept[b, 5].long()
+        assert torch.equal(V[38000 + b, 5, :40], V[ids[b].long()[src // page], 5, src % page])
+
+
+def test_attention_captured_replayed_and_on_two_streams(attnw, variant):
+    pairs = [(1, 1000), (1, 77), (40, 300)] if variant != "few" else [(1, 1000), (1, 77), (2, 300)]
+    c = Paged(pairs, 2, 64, 16, seed=9)
+    Q, scale = c.normal(c.tokens, 8, 64), 0.125
+    mass = torch.zeros(3, 2, c.width * 16, device="cuda")
+    call = lambda q, m: attnw.attn_paged(q, c.K, c.V, c.table, c.lengths, c.starts, scale, mass=m)  # noqa: E731
+    want = call(Q, mass)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graphs, results, queries = [], [], []
+    for _ in range(2):
+        q = Q.clone()
+        with torch.cuda.stream(stream):
+            call(q, mass)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            results.append(call(q, mass))
+        graphs.append(g)
+        queries.append(q)
+    queries[1].mul_(-1)
+    other = call(queries[1], mass)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(20):  # the graphs side by side, and with a plain call
+        for r in results:
+            r[0].fill_(7.0)
+            r[1].fill_(7.0)
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+        with torch.cuda.stream(stream):
+            plain = call(Q, mass)
+        torch.cuda.synchronize()
+        for got, ref in zip((*results, plain), (want, other, want)):
+            assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    # replays read the lengths and the table as they are then
+    c.lengths[0], c.lengths[1] = 500, 64
+    c.K[c.table[2, 0].long()] = 0.5
+    ref = call(Q, mass)
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(results[0][0], ref[0]) and torch.equal(results[0][1], ref[1])
+    # a stream given by its handle, the caller's memory
+    O, m = torch.empty_like(Q), mass.clone()
+    torch.cuda.synchronize()
+    attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, scale, O=O, mass=m, mass_out=m, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(O, ref[0]) and torch.equal(m, ref[1])
+
+
+def test_the_other_calls_captured(attnw):
+    c = Paged([(2, 70), (1, 40)], 2, 64, 16, seed=8, spare=8)
+    f = attnw.rope_frequencies(64).cuda()
+    pos = torch.tensor([68, 69, 39], dtype=torch.int32, device="cuda")
+    q, k, v = c.normal(3, 4, 64), c.normal(3, 2, 64), c.normal(3, 2, 64)
+    mass = torch.rand(2, 2, c.width * 16, device="cuda")
+    out = torch.tensor(c.spare[:6], dtype=torch.int32, device="cuda").view(2, 3)
+    x, xpos = c.normal(1, 4, 9, 64), torch.arange(9, dtype=torch.int32, device="cuda")[None]
+
+    def run():
+        return (attnw.rope(x, xpos, f), attnw.cache_append(q, k, v, c.K, c.V, c.table, c.lengths, c.starts, pos, f),
+                *attnw.cache_evict(c.K, c.V, c.table, c.lengths, mass, 33, 5, table_out=out))
+
+    want = [t.clone() for t in run()]
+    K, V = c.K.clone(), c.V.clone()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        got = run()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        c.K[out[:, :2].long()], c.V[out[:, :2].long()] = 0.0, 0.0  # (pages that the call fills)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(c.K.view(torch.int16), K.view(torch.int16)) and torch.equal(c.V.view(torch.int16), V.view(torch.int16))
+
+
+def test_results_do_not_change_from_call_to_call(attnw, variant):
+    c = Paged([(1, 4000), (1, 900), (1, 2500)] if variant == "few" else [(300, 4000), (1, 900), (1, 2500), (129, 700)], 2, 128, 16, seed=12)
+    Q = c.normal(c.tokens, 8, 128)
+    mass = torch.rand(len(c.pairs), 2, c.width * 16, device="cuda")
+    first = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, 0.1, mass=mass)
+    for _ in range(50):
+        again = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, 0.1, mass=mass)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+
+
+def test_launches_behind_a_failure_write_nothing(attnw):
+    c = Paged([(1, 2000), (200, 900), (0, 40), (2, 0)], 2, 64, 16, seed=6)
+    Q = c.normal(c.tokens, 8, 64)
+    O, lse = torch.full((c.tokens, 8, 64), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((c.tokens, 8), 7.0, device="cuda")
+    mass, out = torch.zeros(4, 2, c.width * 16, device="cuda"), torch.full((4, 2, c.width * 16), 7.0, device="cuda")
+    call = lambda: attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, 0.125, O=O, lse=lse, mass=mass, mass_out=out)  # noqa: E731
+    attnw.set_paged_variant("tensor_cores")
+    try:
+        attnw.selftest_wait_timeout(100000)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            call()
+        torch.cuda.synchronize()
+        assert all(bool((t == 7.0).all()) for t in (O, lse, out))
+        assert attnw.query_status() & 0x80000000
+        call()
+        torch.cuda.synchronize()
+        assert attnw.query_status() == 0 and not bool((O == 7.0).all(-1).any())
+    finally:
+        attnw.set_paged_variant("auto")
 
 
 # ---- eviction -------------------------------------------------------------------------------------------------------------------
