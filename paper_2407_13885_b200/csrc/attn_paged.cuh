@@ -931,7 +931,8 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 
 // Joins the parts of the blocks that stretches of attn_paged_kernel's CTAs cut: O = sum_s 2^(mb_s - top) O_s / sum_s 2^(mb_s - top) l_s, in the order of
 // the parts.  CTA (c, y): the block whose last part CTA c + 1 had, and of its rows a share.  Where a block has few rows (decoding) several warps take a row's parts in turn.
-constexpr int kJoinWarps = 16;
+constexpr int kJoinWarps = 8;
+constexpr int kJoinRows = 4;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32)
@@ -950,60 +951,27 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
     }
     __syncthreads();
     const int rows = x.tokens * shape.group;
-    int each = 1;  // warps a row
-    while (each < kJoinWarps && 2 * each * rows <= kJoinWarps && 4 * each < x.parts) each *= 2;
-    const int per_turn = kJoinWarps / each, mine = warp / each, share = warp % each;
-    for (int r0 = static_cast<int>(blockIdx.y) * per_turn; r0 < rows; r0 += static_cast<int>(gridDim.y) * per_turn) {
-        const int r = r0 + mine;
-        float top = -3.0e38f, l = 0.0f, v[kCols] = {};
-        if (r < rows) {
-            constexpr int kFlight = 4;
-            for (int i0 = share; i0 < x.parts; i0 += kFlight * each) {
-                float2 st[kFlight];
-                float o[kFlight][kCols];
+    // A part's offset and sum, and this lane's columns of its O, into what a row has so far.
+    auto add = [](float2 st, const float (&o)[kCols], float& top, float& l, float (&v)[kCols]) {
+        if (!(st.y > 0.0f)) return;
+        const float next = l > 0.0f ? fmaxf(top, st.x) : st.x;
+        const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(st.x - next);
+        top = next;
+        l = l * f_before + st.y * f_new;
 #pragma unroll
-                for (int f = 0; f < kFlight; ++f) {
-                    const int i = i0 + f * each;
-                    st[f] = make_float2(0.0f, 0.0f);
-                    const int slot = i < x.parts ? slot_of[i] : 2;
-                    if (slot == 2) continue;
-                    const size_t at = static_cast<size_t>(2 * (x.first + i) + slot) * shape.part_rows + r;
-                    st[f] = part_stats[at];
-                    const float* src = part_o + at * D + lane * kCols;
+        for (int c = 0; c < kCols; ++c) v[c] = fmaf(o[c], f_new, v[c] * f_before);
+    };
+    auto load = [&](int i, int r, float2& st, float (&o)[kCols]) {
+        const int slot = i < x.parts && r < rows ? slot_of[i] : 2;
+        st = make_float2(0.0f, 0.0f);
+        if (slot == 2) return;
+        const size_t at = static_cast<size_t>(2 * (x.first + i) + slot) * shape.part_rows + r;
+        st = part_stats[at];
+        const float* src = part_o + at * D + lane * kCols;
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) o[f][c] = src[c];
-                }
-#pragma unroll
-                for (int f = 0; f < kFlight; ++f) {
-                    if (!(st[f].y > 0.0f)) continue;
-                    const float next = l > 0.0f ? fmaxf(top, st[f].x) : st[f].x;
-                    const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(st[f].x - next);
-                    top = next;
-                    l = l * f_before + st[f].y * f_new;
-#pragma unroll
-                    for (int c = 0; c < kCols; ++c) v[c] = fmaf(o[f][c], f_new, v[c] * f_before);
-                }
-            }
-        }
-        if (each > 1) {  // (then there is one turn: rows <= per_turn)
-            sums[warp][32 * kCols] = top;
-            sums[warp][32 * kCols + 1] = l;
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = v[c];
-            __syncthreads();
-            if (share > 0) continue;
-            for (int w = warp + 1; w < warp + each; ++w) {
-                const float l_w = sums[w][32 * kCols + 1], top_w = sums[w][32 * kCols];
-                if (!(l_w > 0.0f)) continue;
-                const float next = l > 0.0f ? fmaxf(top, top_w) : top_w;
-                const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(top_w - next);
-                top = next;
-                l = l * f_before + l_w * f_new;
-#pragma unroll
-                for (int c = 0; c < kCols; ++c) v[c] = fmaf(sums[w][lane * kCols + c], f_new, v[c] * f_before);
-            }
-        }
-        if (r >= rows) continue;
+        for (int c = 0; c < kCols; ++c) o[c] = src[c];
+    };
+    auto store = [&](int r, float top, float l, const float (&v)[kCols]) {
         const int token = r / shape.group, g = r - token * shape.group;
         const size_t out_row = static_cast<size_t>(x.token0 + token) * shape.heads + x.h * shape.group + g;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -1012,7 +980,63 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
         for (int c = 0; c < kCols; c += 2) *reinterpret_cast<uint32_t*>(dst + c) = ptx::pack_bf16x2(v[c] * inv, v[c + 1] * inv);
         if (lane == 0)
             store_lse(cache, shape, lse, lse2, out_row, x.q_tile + token / shape.tile_tokens, x.h, token % shape.tile_tokens * shape.group + g, top, l);
+    };
+    int each = 1;  // warps a row
+    while (each < kJoinWarps && 2 * each * rows <= kJoinWarps && 4 * each < x.parts) each *= 2;
+    if (each == 1) {
+        // a warp takes kJoinRows rows at once, two parts (most blocks have no more) of each on their way
+        for (int r0 = (static_cast<int>(blockIdx.y) * kJoinWarps + warp) * kJoinRows; r0 < rows; r0 += static_cast<int>(gridDim.y) * kJoinWarps * kJoinRows) {
+            float top[kJoinRows], l[kJoinRows], v[kJoinRows][kCols];
+#pragma unroll
+            for (int k = 0; k < kJoinRows; ++k) {
+                top[k] = -3.0e38f;
+                l[k] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) v[k][c] = 0.0f;
+            }
+            for (int i = 0; i < x.parts; i += 2) {
+                float2 st[2][kJoinRows];
+                float o[2][kJoinRows][kCols];
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int k = 0; k < kJoinRows; ++k) load(i + f, r0 + k, st[f][k], o[f][k]);
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int k = 0; k < kJoinRows; ++k) add(st[f][k], o[f][k], top[k], l[k], v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kJoinRows; ++k)
+                if (r0 + k < rows) store(r0 + k, top[k], l[k], v[k]);
+        }
+        return;
     }
+    if (blockIdx.y > 0) return;  // few rows: the first CTA has all of them
+    const int r = warp / each, share = warp % each;
+    float top = -3.0e38f, l = 0.0f, v[kCols] = {};
+    constexpr int kFlight = 4;
+    for (int i0 = share; i0 < x.parts; i0 += kFlight * each) {
+        float2 st[kFlight];
+        float o[kFlight][kCols];
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) load(i0 + f * each, r, st[f], o[f]);
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) add(st[f], o[f], top, l, v);
+    }
+    sums[warp][32 * kCols] = top;
+    sums[warp][32 * kCols + 1] = l;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) sums[warp][lane * kCols + c] = v[c];
+    __syncthreads();
+    if (share > 0 || r >= rows) return;
+    for (int w = warp + 1; w < warp + each; ++w) {
+        float o[kCols];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) o[c] = sums[w][lane * kCols + c];
+        add(make_float2(sums[w][32 * kCols], sums[w][32 * kCols + 1]), o, top, l, v);
+    }
+    store(r, top, l, v);
 }
 
 }  // namespace pa

@@ -255,7 +255,7 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
                                       shape, starts, scale_log2e, o, lse, lse2, part, stats, joins);
     if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && part && ctas > 1) {
-        const unsigned slices = static_cast<unsigned>((w.part_rows + 4 * pa::kJoinWarps - 1) / (4 * pa::kJoinWarps));
+        const unsigned slices = static_cast<unsigned>((w.part_rows + pa::kJoinRows * pa::kJoinWarps - 1) / (pa::kJoinRows * pa::kJoinWarps));
         e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, part, stats, joins, o,
                                  lse, lse2);
         if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
