@@ -111,22 +111,33 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
         }
     };
     ptx::grid_dependency_wait();
-    int b, t0, t1, end;
+    int b, t0, t1, end, length;
     if (WEIGH) {
         b = item / cache.kv_heads;
         const int s0 = starts[b];
         end = starts[b + 1];
+        length = paged::length_of(cache, b);
         t0 = min(max(s0, 0), shape.tokens);
         t1 = min(max(end, 0), shape.tokens);
     } else {
-        paged::sample_starts(&samples, starts, cache.sequences, kThreads);
-        __syncthreads();
         t0 = item / cache.kv_heads;
-        b = paged::owner_of(&samples, starts, cache.sequences, t0, &end);
-        if (b < 0) return;  // (all CTAs of the cluster)
         t1 = t0 + 1;
+        if (cache.sequences <= 32) {  // a lane a sequence: one latency for all that is asked
+            const bool there = lane < cache.sequences;
+            const int from = there ? starts[lane] : 0, to = there ? starts[lane + 1] : 0, of_lane = there ? paged::length_of(cache, lane) : 0;
+            const uint32_t owners = __ballot_sync(0xffffffffu, there && from <= t0 && t0 < to);
+            if (owners == 0u) return;  // (all CTAs of the cluster)
+            b = 31 - __clz(owners);
+            end = __shfl_sync(0xffffffffu, to, b);
+            length = __shfl_sync(0xffffffffu, of_lane, b);
+        } else {
+            paged::sample_starts(&samples, starts, cache.sequences, kThreads);
+            __syncthreads();
+            b = paged::owner_of(&samples, starts, cache.sequences, t0, &end);
+            if (b < 0) return;
+            length = paged::length_of(cache, b);
+        }
     }
-    const int length = paged::length_of(cache, b);
     const int capacity = cache.table_width << cache.page_shift;
     const size_t mass_row = (static_cast<size_t>(b) * cache.kv_heads + h) * capacity;
     // This CTA's units of the sequence's keys, the same for all its tokens.

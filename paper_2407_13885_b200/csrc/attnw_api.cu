@@ -86,6 +86,7 @@ struct DeviceInfo {
     cudaEvent_t fork_event = nullptr, join_event = nullptr;
     std::atomic<int> gridrow_clusters[2][2][17] = {};  // resident clusters of 2..16 CTAs of the grid-row kernel, [d == 128][P is float32][CTAs], 0 = not asked yet
     std::atomic<int> attn_clusters[2][5] = {};  // resident clusters of 2 and 4 CTAs of the one-pass attention kernel, [d == 128][CTAs]
+    std::atomic<int> few_clusters[9] = {};  // resident clusters of 2..8 CTAs of attn_few_kernel, 0 = not asked yet
     int rc_clusters[2][17] = {};  // resident clusters of 1..16 CTAs of the register-cluster row kernel, [P is float32][CTAs]
 };
 std::mutex g_split_mutex;

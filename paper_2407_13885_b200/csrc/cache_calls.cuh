@@ -276,27 +276,57 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
     return ATTNW_OK;
 }
 
+// How many clusters of `ctas` CTAs of attn_few_kernel the device holds at once, one CTA an SM; at least 1.
+int few_max_clusters(DeviceInfo* dev, int ctas) {
+    if (ctas == 1) return dev->sm_count;
+    std::atomic<int>& memo = dev->few_clusters[ctas];
+    int n = memo.load(std::memory_order_relaxed);
+    if (n != 0) return n;
+    constexpr auto kernel = few::attn_few_kernel<128, 4, true>;  // (of the largest; where others fit twice, twice as many do)
+    const int bytes = few::Smem<128, 4>::bytes(few::kMaxScores / 5 / few::kUnit * few::kUnit, true);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(ctas);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(few::kThreads, 1, 1);
+    cfg.gridDim = dim3(static_cast<unsigned>(ctas * dev->sm_count), 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (allow_smem<few::attn_few_kernel<128, 4, true>>(bytes) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+        (void)cudaGetLastError();
+        n = 1;
+    }
+    memo.store(n, std::memory_order_relaxed);
+    return n;
+}
+
 // How attn_few_kernel would serve a call.
 struct FewShape {
     int gp = 0;  // heads of the group, rounded up to a power of two; 0: it does not
-    int cluster = 1, max_keys = 0, smem = 0;
+    int cluster = 1, max_keys = 0;
+    long long rounds = 0;  // of clusters
 };
-template <int D, int GP>
-constexpr int few_bytes(int max_keys, bool weigh) { return few::Smem<D, GP>::bytes(max_keys, weigh); }
-FewShape few_shape(const attnw_cache* c, int tokens, int heads, bool weigh, int sm_count) {
+FewShape few_shape(DeviceInfo* dev, const attnw_cache* c, int tokens, int heads, bool weigh) {
     FewShape f;
     const int group = heads / c->kv_heads;
     if (group > 8) return f;
     int gp = 1;
     while (gp < group) gp *= 2;
-    // A cluster of as many CTAs as fill the device once, each with 64 keys at least.
+    // The largest clusters that all fit at once, of 64 keys a CTA at least: a second round costs as much as the first (one over 2000, 8 heads on
+    // 8, d = 64: clusters of 1 ... 6 11.2 ... 6.6 us, of 8, of which 15 fit and 16 are needed, 10.7).
     const long long capacity = static_cast<long long>(c->table_width) * c->page, items = static_cast<long long>(weigh ? c->sequences : tokens) * c->kv_heads;
     if (items * few::kMaxCluster > INT_MAX) return f;
-    f.cluster = static_cast<int>(std::max(1ll, std::min({static_cast<long long>(few::kMaxCluster), sm_count / items, capacity / 64})));
+    f.cluster = few::kMaxCluster;
+    while (f.cluster > 1 && (capacity < 64ll * f.cluster || items > few_max_clusters(dev, f.cluster))) --f.cluster;
     auto keys_of = [&](int cluster) { return ((capacity + few::kUnit - 1) / few::kUnit + cluster - 1) / cluster * few::kUnit; };
     while (f.cluster < few::kMaxCluster && keys_of(f.cluster) * (gp + 1) > few::kMaxScores) ++f.cluster;
     if (keys_of(f.cluster) * (gp + 1) > few::kMaxScores) return f;
     f.max_keys = static_cast<int>(keys_of(f.cluster));
+    const int at_once = few_max_clusters(dev, f.cluster);
+    f.rounds = (items + at_once - 1) / at_once;
     f.gp = gp;
     return f;
 }
@@ -326,19 +356,18 @@ cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void
     return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, stream);
 }
 
-// Is it the faster one?  Its time goes by the bytes that an SM reads, 27 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
-// other one's by the bytes in all, which it spreads evenly, after 12 us (one wave of short blocks) to 25 (cut ones, joined), and with weights 20
-// more.  The lengths are on the device: caches count as full.  us per call, few -> tensor cores, 32 heads on 8, d = 128: one token over 100 keys 7.3 / 12.6,
-// 1000 8.9 / 24.7, 4000 13.1 / 24.2, 16000 33.6 / 26.5, 4 over 4000 21.2 / 27.8, 16 over 1000 20.1 / 26.9, 16 tokens of one sequence over 500
-// 20.2 / 17.5; 64 heads on 8, 8 tokens over 4000 72 / 42; 8 heads on 8 31 / 42.  With weights: 1 over 1000 10.3 / 36.2, 16000 35 / 48, 32 over 4095 145 / 202, 64
-// heads on 8, 8 over 4000 81 / 75; four tokens of one sequence over 100 27 / 23.
-bool few_pays(const attnw_cache* c, const FewShape& f, int tokens, bool weigh, int sm_count) {
+// Is it the faster one?  Its time goes by the bytes that a CTA reads, 27 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
+// other one's by the bytes in all, which it spreads evenly, after 12 us (blocks that are not cut) to 25 (cut ones, joined), and with weights 10 to 20
+// more.  The lengths are on the device: caches count as full.  us per call, few -> tensor cores, 32 heads on 8, d = 128: one token over 100 keys 6.9 / 12.6,
+// 1000 8.5 / 26.9, 4000 12.7 / 24.1, 16000 32.6 / 26.4, 4 over 4000 20.7 / 28.0, 16 over 1000 19.4 / 28.3, 16 tokens of one sequence over 500
+// 12.4 / 17.7, 8 each of four over 1000 32.9 / 28.0; 64 heads on 8, 8 tokens over 4000 69 / 44; 8 heads on 8 30 / 42.  With weights: 1 over 1000 10.3 / 36.4,
+// 16000 35 / 46, 32 over 4095 145 / 225, 64 heads on 8, 8 over 4000 81 / 75; four tokens of one sequence over 100 26.9 / 20.4.
+bool few_pays(const attnw_cache* c, const FewShape& f, int tokens, bool weigh) {
     if (weigh && tokens > c->sequences) return false;  // (a sequence's tokens take turns there)
-    const long long ctas = static_cast<long long>(weigh ? c->sequences : tokens) * c->kv_heads * f.cluster, waves = (ctas + sm_count - 1) / sm_count;
     long long most = f.gp <= 2 ? 1024 : f.gp == 4 ? 512 : 256;  // kB
     if (weigh) most = f.gp <= 4 ? 4096 : 768;
-    if (tokens > c->sequences) most /= 2;
-    return waves * (f.max_keys * 4ll * c->d / 1024 + 128) <= most + 128;
+    if (tokens > c->sequences) most = most * 3 / 4;  // (the other one reads a sequence's keys once for all its tokens)
+    return f.rounds * (f.max_keys * 4ll * c->d / 1024 + 128) <= most + 128;
 }
 
 int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
@@ -374,9 +403,9 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     rc = current_device(&dev);
     if (rc != ATTNW_OK) return rc;
     const int variant = g_paged_variant.load(std::memory_order_relaxed);
-    const FewShape f = variant == 1 ? FewShape{} : few_shape(c, tokens, heads, mass != nullptr, dev->sm_count);
+    const FewShape f = variant == 1 ? FewShape{} : few_shape(dev, c, tokens, heads, mass != nullptr);
     if (variant == 2 && f.gp == 0) return ATTNW_ERR_UNSUPPORTED;
-    if (f.gp > 0 && (variant == 2 || few_pays(c, f, tokens, mass != nullptr, dev->sm_count))) {
+    if (f.gp > 0 && (variant == 2 || few_pays(c, f, tokens, mass != nullptr))) {
         const auto launch = c->d == 64 ? (mass ? launch_few_group<64, true> : launch_few_group<64, false>)
                                        : (mass ? launch_few_group<128, true> : launch_few_group<128, false>);
         if (launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
