@@ -489,7 +489,18 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 ++q_loads;
             };
             // Both kinds in the order of the keys (split: the units take them in turn), each as soon as it has room.
-            int k = 0, v = 0, where_k = place(tile0), where_v = where_k;
+            // The table is asked four tiles ahead: its answer takes 600 cycles, as long as a tile's boxes take to issue.
+            constexpr int kAhead = 4;
+            int k = 0, v = 0, where_k[kAhead], where_v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) where_k[i] = place(tile0 + i);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) where_v[i] = where_k[i];
+            auto advance = [&](int (&where)[kAhead], int next) {
+#pragma unroll
+                for (int i = 0; i + 1 < kAhead; ++i) where[i] = where[i + 1];
+                where[kAhead - 1] = place(tile0 + next + kAhead - 1);
+            };
             long long idle_since = 0;
             bool q_here = false;
             auto ready = [&](size_t barrier, const Entry& e) { return __all_sync(0xffffffffu, ptx::mbar_test_wait(bar_of(barrier, e.stage), e.phase ^ 1u)); };
@@ -502,18 +513,18 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             while (ok && v < tiles) {
                 bool idle = true;
                 if (k < tiles && ready(offsetof(Barriers, k_empty), ek)) {
-                    load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), smem + L::kKOff + ek.stage * L::kTileBytes, tile0 + k, where_k);
+                    load(&tm_k, bar_of(offsetof(Barriers, k_full), ek.stage), smem + L::kKOff + ek.stage * L::kTileBytes, tile0 + k, where_k[0]);
                     ek.next(L::kStages);
                     ++k_loads;
                     if (!q_here) load_queries();
-                    where_k = place(tile0 + ++k);
+                    advance(where_k, ++k);
                     idle = false;
                 }
                 if (ok && v < k && ready(offsetof(Barriers, v_empty), ev)) {
-                    load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), smem + L::kVOff + ev.stage * L::kTileBytes, tile0 + v, where_v);
+                    load(&tm_v, bar_of(offsetof(Barriers, v_full), ev.stage), smem + L::kVOff + ev.stage * L::kTileBytes, tile0 + v, where_v[0]);
                     ev.next(L::kStages);
                     ++v_loads;
-                    where_v = place(tile0 + ++v);
+                    advance(where_v, ++v);
                     idle = false;
                 }
                 if (!idle) {
