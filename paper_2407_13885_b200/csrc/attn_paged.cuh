@@ -37,6 +37,7 @@ constexpr int kRoles = 19;       // warps that work on segments
 // Costs are in keys of one query tile (two query tiles: twice that).
 constexpr int kBlockCost = 2 * kTile;                // of a block besides: its set-up and its result
 constexpr int kLeastCost = kBlockCost + 4 * kTile;   // of a CTA's stretch
+constexpr int kLeastEven = 4 * kTile, kFewBlocks = 18;  // where blocks begin with a stretch (Walk::find)
 constexpr int kLeastCut = 8;                         // key tiles of a block that may be cut
 constexpr int kSlots = 4;                            // segments on their way from the scheduler to the others
 
@@ -171,9 +172,9 @@ __device__ __forceinline__ long long divided(long long a, long long b) {
     return (a | b) >> 32 == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
 
-// How many of a block's key tiles lie in front of stretch `index`: the block begins at `begin`, has `all` tiles, each of 2^shift keys' cost.
-__device__ __forceinline__ int tiles_in_front(long long index, long long stretch, long long begin, int all, int shift) {
-    const long long into = index * stretch - begin - kBlockCost;
+// How many of a block's key tiles lie in front of stretch `index`: its keys begin at `keys`, and it has `all` tiles, each of 2^shift keys' cost.
+__device__ __forceinline__ int tiles_in_front(long long index, long long stretch, long long keys, int all, int shift) {
+    const long long into = index * stretch - keys;
     if (into <= 0) return 0;
     const long long t = (into + (1ll << shift) - 1) >> shift;
     if (t >= all) return all;
@@ -187,7 +188,7 @@ struct Join {
     int b, h, token0, tokens, q_tile;
     int first, parts;  // the CTA with the first part; those from it to the last one's, 0: there is nothing to join
     int all, shift;    // (tiles_in_front)
-    long long begin, stretch;
+    long long keys, stretch;
 };
 
 // A warp's way along the row of all blocks: sequence by sequence, key head by key head, block by block.  Lane i has the share of sequence
@@ -196,6 +197,7 @@ struct Walk {
     int lane, b0 = 0;
     Share mine;
     long long stretch;  // cost of a CTA's
+    bool even;          // every block begins with a stretch, and costs whole ones
     // the block at hand
     int b = -1, h = 0, r = 0, q_tile0 = 0;  // b < 0: behind the last
     Share share;
@@ -217,19 +219,29 @@ struct Walk {
     // The cost of everything, and the block that `index` stretches behind the beginning lies in.
     __device__ __forceinline__ void find(const paged::Cache& c, const Shape& s, const int* starts, long long index) {
         lane = static_cast<int>(threadIdx.x & 31);
-        long long total = 0;
+        long long total = 0, blocks = 0;
+        bool many = false;
         for (b0 = 0; b0 < c.sequences; b0 += 32) {
             load(c, s, starts);
             total += mine.cost_upto(s, mine.blocks) * c.kv_heads;
+            blocks += static_cast<long long>(mine.blocks) * c.kv_heads;
+            many = many || mine.blocks > 1;
         }
         total = warp_sum(total);
+        blocks = warp_sum(blocks);
         stretch = max(static_cast<long long>(kLeastCost), divided(total + s.ctas - 1, s.ctas));
+        // Few blocks: a CTA's way from one to the next takes as long as several key tiles, so none has parts of two.  Rounded up to whole stretches
+        // they take at most a stretch more each.  (us per call, 32 heads on 8, d = 128, one token over 4000 keys, 8 blocks: 24.1 -> 20.0; not with more: 4
+        // tokens, 32 blocks, 28.0 -> 31.9.)
+        even = !__any_sync(0xffffffffu, many) && blocks <= kFewBlocks && 2 * blocks <= s.ctas;
+        if (even) stretch = max(static_cast<long long>(kLeastEven), divided(total + (s.ctas - blocks) - 1, s.ctas - blocks));
         const long long at = index * stretch;
         long long first = 0;
         int q_first = 0;
         for (b0 = 0; b0 < c.sequences; b0 += 32) {
             if (c.sequences > 32) load(c, s, starts);  // (else they are at hand)
-            const long long a_head = mine.cost_upto(s, mine.blocks), cost = a_head * c.kv_heads;
+            const long long a_head = even ? (mine.blocks > 0 ? rounded(mine.seen_of(s, 0) * weight_of(s, mine, 0)) : 0) : mine.cost_upto(s, mine.blocks);
+            const long long cost = a_head * c.kv_heads;
             const long long end = first + warp_scan(cost, lane);
             const int q_tiles = q_tiles_of(s, mine), q_end = q_first + static_cast<int>(warp_scan(q_tiles, lane));
             const uint32_t here = __ballot_sync(0xffffffffu, at >= end - cost && at < end);
@@ -241,6 +253,10 @@ struct Walk {
                 const long long seq_begin = __shfl_sync(0xffffffffu, end - cost, from), of_head = __shfl_sync(0xffffffffu, a_head, from);
                 h = static_cast<int>(divided(at - seq_begin, of_head));
                 begin = seq_begin + h * of_head;
+                if (even) {
+                    r = 0;
+                    return;
+                }
                 int lo = 0, hi = share.blocks;  // cost_upto(lo) <= at - begin < cost_upto(hi)
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
@@ -255,7 +271,8 @@ struct Walk {
         }
     }
     __device__ __forceinline__ void next(const paged::Cache& c, const Shape& s, const int* starts) {
-        begin += kBlockCost + static_cast<long long>(weight(s)) * share.seen_of(s, r);
+        const long long keys = static_cast<long long>(weight(s)) * share.seen_of(s, r);
+        begin += even ? rounded(keys) : kBlockCost + keys;
         if (++r < share.blocks) return;
         r = 0;
         if (++h < c.kv_heads) return;
@@ -279,10 +296,13 @@ struct Walk {
             from = 0;
         }
     }
-    __device__ __forceinline__ int weight(const Shape& s) const { return share.tokens_of(s, r) > s.tile_tokens ? 2 : 1; }
+    __device__ __forceinline__ static int weight_of(const Shape& s, const Share& x, int r) { return x.tokens_of(s, r) > s.tile_tokens ? 2 : 1; }
+    __device__ __forceinline__ int weight(const Shape& s) const { return weight_of(s, share, r); }
+    __device__ __forceinline__ long long rounded(long long cost) const { return max(1ll, divided(cost + stretch - 1, stretch)) * stretch; }
+    __device__ __forceinline__ long long keys() const { return begin + (even ? 0 : kBlockCost); }
     __device__ __forceinline__ int tiles(const Shape& s) const { return (share.seen_of(s, r) + kTile - 1) / kTile; }
     __device__ __forceinline__ int tiles_before(const Shape& s, long long index) const {
-        return tiles_in_front(index, stretch, begin, tiles(s), weight(s) == 2 ? 8 : 7);
+        return tiles_in_front(index, stretch, keys(), tiles(s), weight(s) == 2 ? 8 : 7);
     }
 };
 
@@ -409,7 +429,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 const int i0 = walk.r * 2 * shape.tile_tokens;
                 if (first_block && t0 > 0 && t0 < t1 && t1 == all)  // the last part of a block that began in front
                     join = {walk.b, walk.h, walk.share.token0 + i0, walk.share.tokens_of(shape, walk.r), walk.q_tile0 + 2 * walk.r,
-                            -1, 0, all, walk.weight(shape) == 2 ? 8 : 7, walk.begin, walk.stretch};
+                            static_cast<int>(divided(walk.begin, walk.stretch)), 0, all, walk.weight(shape) == 2 ? 8 : 7, walk.keys(), walk.stretch};
                 first_block = false;
                 if (t0 < t1 || (all == 0 && walk.begin >= cta * walk.stretch)) {
                     s.b = walk.b;
@@ -439,10 +459,7 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             walk.next(cache, shape, starts);
         }
         if (joins && lane == 0) {
-            if (join.all > 0) {
-                join.first = static_cast<int>(divided(join.begin, join.stretch));
-                join.parts = static_cast<int>(cta) - join.first + 1;
-            }
+            if (join.all > 0) join.parts = static_cast<int>(cta) - join.first + 1;
             joins[cta] = join;
         }
     } else if (warp == kProducer) {
@@ -957,7 +974,7 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
     const Join x = joins[blockIdx.x + 1];
     if (*reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u || x.parts == 0) return;
     for (int i = static_cast<int>(threadIdx.x); i < x.parts; i += kJoinWarps * 32) {
-        const int t0 = tiles_in_front(x.first + i, x.stretch, x.begin, x.all, x.shift), t1 = tiles_in_front(x.first + i + 1, x.stretch, x.begin, x.all, x.shift);
+        const int t0 = tiles_in_front(x.first + i, x.stretch, x.keys, x.all, x.shift), t1 = tiles_in_front(x.first + i + 1, x.stretch, x.keys, x.all, x.shift);
         slot_of[i] = t0 >= t1 ? 2 : t0 > 0 ? 0 : 1;
     }
     __syncthreads();

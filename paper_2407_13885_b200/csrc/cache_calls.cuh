@@ -240,10 +240,10 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
         return ATTNW_ERR_CUDA;
     }
     const paged::Cache view = view_of(c);
-    // As many CTAs as may have something to do: the most that all blocks can cost, by stretches of the least cost.
+    // As many CTAs as may have something to do: the most that all blocks can cost, by the shortest stretches.
     const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(std::min(c->sequences, tokens))) * c->kv_heads;
     const long long capacity = static_cast<long long>(c->table_width) * c->page, most = blocks * (pa::kBlockCost + capacity * (tokens > tile_tokens ? 2 : 1));
-    const int ctas = static_cast<int>(std::min({static_cast<long long>(kPagedCtas), static_cast<long long>(sm_count), (most + pa::kLeastCost - 1) / pa::kLeastCost}));
+    const int ctas = static_cast<int>(std::min({static_cast<long long>(kPagedCtas), static_cast<long long>(sm_count), (most + pa::kLeastEven - 1) / pa::kLeastEven}));
     const pa::Shape shape{tokens, heads, group, tile_tokens, w.part_rows, w.q_tiles, ctas};
     auto* stats = w.part_rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
     auto* joins = w.part_rows > 0 ? reinterpret_cast<pa::Join*>(workspace + w.joins) : nullptr;
