@@ -1,7 +1,7 @@
 // Attention of few new tokens over a paged cache: decoding over caches that are short, or where each key is wanted once.
 //
-// The operation is attn_paged_kernel's (attn_paged.cuh), which spends some 12 us on its way through tensor memory however little there is to do, 5 more on
-// joining cut blocks, and reads the keys a second time for their weights.  Here a cluster of up to 8 CTAs has one token's (or one
+// The operation is attn_paged_kernel's (attn_paged.cuh), which spends some 12 us on its way through tensor memory however little there is to do, 8 more
+// where blocks are cut and joined, and reads the keys a second time for their weights.  Here a cluster of up to 8 CTAs has one token's (or one
 // sequence's) key head: each takes a range of the keys, dots them with the queries of the group on the FMA pipes, keeps the scores in shared
 // memory, turns them into 2^(c s - m) with its own maximum m, adds up the values, and the CTAs join their parts through distributed shared
 // memory.  What a key weighs is then there to be added to `mass`: one launch in all.
@@ -9,7 +9,10 @@
 // A warp reads 8 or 16 keys at a time (of one page: pages are multiples of 16), four 16-byte vectors a lane, and the next ones while it works on
 // them; the queries stay in registers; the dot products are reduced over a key's lanes by halves, heads first, so that 4 heads over 8 lanes
 // take 4 shuffles and not 12.
-// Bound: the latency of a chain of loads (lengths, table, keys, values) for small calls, HBM for large ones.
+// Bound: the latency of a chain of loads (lengths, table, keys, values) for small calls (one token over 500 keys, 12 heads, d = 64: 5.2 us); for larger
+// ones each warp's own instructions, of which a key takes as many as there are heads (8 sequences of up to 4096 keys, 32 heads on 8, d = 128, with
+// weights: 35.3 us, where the 65 MB take 9.9 and half of the CTAs have long been done: a cluster is as slow as the longest sequence).  A ring of
+// asynchronous copies with three turns on their way helped one head a group (30 -> 25.5 us), and cost four (16 tokens over 1000 keys 19.4 -> 21.7).
 #pragma once
 #include "attnw_fused.cuh"
 #include "paged.cuh"

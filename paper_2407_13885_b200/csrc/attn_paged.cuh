@@ -15,6 +15,10 @@
 // and each works out for itself what it does: all blocks lie in a row, each as long as it costs, and the CTA has a stretch of it (Walk).  It may
 // begin and end inside a block: then its unnormalised O, offset and sum go to a workspace, and combine_kernel joins them.  A CTA
 // goes through its blocks without a stop: while its Softmax warps finish one, the tiles of the next arrive.
+//
+// Bound: HBM for single tokens over long caches (24 over up to 32768 keys, 32 heads on 8, d = 128, 1.8 GB: 283 us, 6.5 TB/s, as fast as a plain copy; 325 in
+// a loop at the power cap).  For chunks tensor pipe and special function units, 1024 cycles each a tile of 128 x 128 at d = 128: 4 x 2048 tokens over some
+// 6000 keys each 690 us, 1.05 PFLOP/s (780 in a loop); the pipe is at 48 %, the rest are hand-overs between the roles and tiles cut by the diagonal.
 #pragma once
 #include <cstddef>
 
