@@ -1,11 +1,14 @@
 """Attention weights ``P = Softmax(scale * Q K^T)`` on B200 (sm_100a).
 
-Two operations, both hand-written CUDA behind a C-ABI shared library (``include/attnw.h``):
+Hand-written CUDA behind a C-ABI shared library (``include/attnw.h``):
 
 * ``attnw_fused`` - matmul, scaling and Softmax in one kernel (the fused kernel of
   Section VII of the paper, re-designed for tcgen05 / TMEM / TMA);
 * ``softmax_rows`` - the dedicated row-Softmax kernel over precomputed scores
-  (Section VI-B).
+  (Section VI-B);
+* ``attn_fused``, ``project_qk`` - the product with V, and the projection in front (in ``binding``, as all that follows);
+* ``rope``, ``cache_append``, ``attn_paged``, ``cache_evict`` - generating token by token: rotary positions, a paged cache,
+  Attention over it with the weight that each key receives, and eviction by that weight.
 
 The Python layer only marshals pointers; there is no CPU or PyTorch fallback - calling an
 operation without the compiled library raises.
