@@ -2,17 +2,20 @@
 //
 // The operation is attn_paged_kernel's (attn_paged.cuh), which spends some 12 us on its way through tensor memory however little there is to do, 8 more
 // where blocks are cut and joined, and reads the keys a second time for their weights.  Here a cluster of up to 8 CTAs has one token's (or one
-// sequence's) key head: each takes a range of the keys, dots them with the queries of the group on the FMA pipes, keeps the scores in shared
+// sequence's) key head: each takes a range of the keys, multiplies them with the queries of the group, keeps the scores in shared
 // memory, turns them into 2^(c s - m) with its own maximum m, adds up the values, and the CTAs join their parts through distributed shared
 // memory.  What a key weighs is then there to be added to `mass`: one launch in all.
 //
-// A warp reads 8 or 16 keys at a time (of one page: pages are multiples of 16), four 16-byte vectors a lane, and the next ones while it works on
-// them; the queries stay in registers; the dot products are reduced over a key's lanes by halves, heads first, so that 4 heads over 8 lanes
-// take 4 shuffles and not 12.
+// Groups of 3 to 8 heads: a warp takes 16 keys (of one page: pages are multiples of 16) at a time, and both products are m16n8k16 products of a warp, whose
+// operands are 16-byte vectors just as they were loaded: neither the order of the features of a score nor that of the keys of a sum matters, so a lane's
+// vector is its share of the operand.  (tcgen05 wants its operands in shared memory and 64 rows at least, and its results take a way of 12 us.)  One or two
+// heads: FMA pipes, four vectors a lane and turn, the dot products reduced over a key's lanes by halves, heads first.  Eight heads' products for one
+// head's cost more than they save: one token over 500 keys, 12 heads on 12, d = 64 the same, 8 tokens over 4000 27 us -> 30.
+// us per call before (FMA pipes for all) -> now: 32 heads on 8, 8 tokens over 4095 keys 35 -> 30.9, 16 over 1000 19.6 -> 16.9, with weights 21.6 -> 19.6,
+// 64 heads on 8, 8 over 4000 71 -> 46, with weights 81 -> 57; 14 heads on 2, d = 64, 32 over 2000 19.3 -> 13.3.
 // Bound: the latency of a chain of loads (lengths, table, keys, values) for small calls (one token over 500 keys, 12 heads, d = 64: 5.2 us); for larger
-// ones each warp's own instructions, of which a key takes as many as there are heads (8 sequences of up to 4096 keys, 32 heads on 8, d = 128, with
-// weights: 35.3 us, where the 65 MB take 9.9 and half of the CTAs have long been done: a cluster is as slow as the longest sequence).  A ring of
-// asynchronous copies with three turns on their way helped one head a group (30 -> 25.5 us), and cost four (16 tokens over 1000 keys 19.4 -> 21.7).
+// ones the loads that a warp has on their way, 4 KB (8 sequences of up to 4096 keys, 32 heads on 8, d = 128, with weights: 30.6 us, where the 65 MB take 9.9
+// and half of the CTAs have long been done: a cluster is as slow as the longest sequence).  More clusters than fit at once were slower at every length.
 #pragma once
 #include "attnw_fused.cuh"
 #include "paged.cuh"
@@ -82,18 +85,31 @@ __device__ __forceinline__ int head_of(int lane) {
     return head;
 }
 
+// D (16 x 8, float32) += A (16 x 16) B (16 x 8), bfloat16, by one warp.  Lane (r, c) = (lane / 4, lane % 4) has of A rows r and r + 8 at k = 2c, 2c + 1
+// (a[0], a[1]) and 2c + 8, 2c + 9 (a[2], a[3]), of B column r at the same k (b0, b1), of D rows r (d[0], d[1]) and r + 8 (d[2], d[3]) in columns 2c, 2c + 1.
+__device__ __forceinline__ void multiply(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
 // Item: without weights (token, key head), with weights (sequence, key head) and its tokens one after the other.
 template <int D, int GP, bool WEIGH>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape,
                 const int* starts, float scale_log2e, __nv_bfloat16* O, float* lse, const float* mass, float* mass_out) {
     using L = Smem<D, GP>;
-    constexpr int kKeyLanes = GP <= 4 ? 8 : D / 8, kVecs = D / 8 / kKeyLanes;  // keys: lanes of a key, vectors of a lane
+    constexpr bool kTensor = GP >= 4;
+    // FMA pipes:
+    constexpr int kKeyLanes = 8, kVecs = D / 8 / kKeyLanes;  // keys: lanes of a key, vectors of a lane
     constexpr int kRowLanes = D / 8;                                            // values: lanes of a key
     constexpr int kKeys = 4 * (32 / kRowLanes);                                  // that a warp takes at a time, four vectors a lane
     constexpr int kTurns = kUnit / kKeys;                                        // of a unit
     constexpr int kHeadLanes = kKeyLanes / GP > 0 ? kKeyLanes / GP : 1;          // lanes that end up with the same sum
     static_assert(kKeys * kKeyLanes * kVecs == 32 * 4 && kKeyLanes >= GP, "four vectors a lane");
+    // Tensor cores:
+    constexpr int kSteps = D / 32;   // of a unit's keys: 32 features, two vectors a lane
+    constexpr int kHalves = D / 64;  // of a unit's values: 64 features, four vectors a lane
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ paged::Samples samples;
     float* part = reinterpret_cast<float*>(smem + L::kPartOff);
@@ -171,58 +187,133 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
     };
     const int my_turns = max(0, unit1 - unit0 - warp + kWarps - 1) / kWarps * kTurns;  // of this warp
     auto turn_begin = [&](int i) { return (warp + kWarps * (i / kTurns)) * kUnit + i % kTurns * kKeys; };  // its first key, from key0 on
+    const int my_units = max(0, unit1 - unit0 - warp + kWarps - 1) / kWarps;  // of this warp
+    const int r = lane >> 2, c = lane & 3;
+    // Unit i of this warp: its page (below 0: none), and the first of its rows.
+    auto rows_of = [&](const __nv_bfloat16* data, int i, int* key) {
+        const int unit = unit0 + warp + kWarps * i;
+        const int page = i < 32 ? __shfl_sync(0xffffffffu, page_mine, i & 31) : unit < unit1 ? paged::page_of(cache.table, cache, b, unit * kUnit) : -1;
+        *key = unit * kUnit;
+        return page >= 0 ? data + paged::row_offset(cache, page, h, *key) : nullptr;
+    };
+    auto vector_of = [&](const __nv_bfloat16* rows, bool there, int at) {
+        return rows != nullptr && there ? __ldcs(reinterpret_cast<const uint4*>(rows + at)) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    // Keys r and r + 8 of the unit, features 8c ... 8c + 7 of each 32; zeros where there is no key that the token sees.
+    auto fetch_keys = [&](int i, int seen, uint4 (&v)[2 * kSteps]) {
+        int key;
+        const __nv_bfloat16* rows = rows_of(cache.K, i, &key);
+#pragma unroll
+        for (int x = 0; x < 2 * kSteps; ++x) v[x] = vector_of(rows, key + r + (x & 1) * 8 < seen, (r + (x & 1) * 8) * D + (x >> 1) * 32 + c * 8);
+    };
+    // Values c, c + 4, c + 8, c + 12 of the unit, features 8r ... 8r + 7 of 64.
+    auto fetch_values = [&](int i, int half, int seen, uint4 (&v)[4]) {
+        int key;
+        const __nv_bfloat16* rows = rows_of(cache.V, i, &key);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = vector_of(rows, key + c + 4 * x < seen, (c + 4 * x) * D + half * 64 + r * 8);
+    };
+    // The values `ahead` units behind unit i of that half, all units of one half in front of the next.
+    auto fetch_next = [&](int i, int half, int ahead, int seen, uint4 (&v)[4]) {
+        int n = i + ahead, y = half;
+        while (n >= my_units && y < kHalves) {
+            n -= my_units;
+            ++y;
+        }
+        if (y < kHalves) fetch_values(n, y, seen, v);
+    };
+    auto unit_begin = [&](int i) { return (warp + kWarps * i) * kUnit; };  // its first key, from key0 on
     const float c2 = scale_log2e;
 
     for (int t = t0; t < t1; ++t) {
         const long long seen_by = static_cast<long long>(length) - (static_cast<long long>(end) - t) + 1;
         const int seen = static_cast<int>(min(max(seen_by, 0ll), static_cast<long long>(length)));
-        uint64_t q[GP][4 * kVecs];  // pairs of features
+        uint4 next[4], values[2][4];  // (of either path; loaded in front of the weights)
+        if constexpr (kTensor) {
+            uint4 q[kSteps];  // head r, features 8c ... 8c + 7 of each 32
 #pragma unroll
-        for (int g = 0; g < GP; ++g)
+            for (int x = 0; x < kSteps; ++x)
+                q[x] = r < shape.group ? *reinterpret_cast<const uint4*>(Q + t * q_token + (h * shape.group + r) * q_head + x * 32 + c * 8) : make_uint4(0u, 0u, 0u, 0u);
+            // ---- scores, and their maximum: keys are the rows, heads the columns; the order of the features is the same for both ----
+            float top[2] = {-3.0e38f, -3.0e38f};  // of heads 2c, 2c + 1
+            uint4 keys[2 * kSteps];
+            if (my_units > 0) fetch_keys(0, seen, keys);
+            for (int i = 0; i < my_units; ++i) {
+                uint4 v[2 * kSteps];
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (g < shape.group)
-                    v = *reinterpret_cast<const uint4*>(Q + t * q_token + (h * shape.group + g) * q_head + (i * kKeyLanes + lane % kKeyLanes) * 8);
-                unpack_pairs(v, q[g] + 4 * i);
-            }
-        // ---- scores, and their maximum ----
-        const int head = head_of<GP, kKeyLanes>(lane);
-        float top = -3.0e38f;
-        uint4 next[4];
-        if (my_turns > 0) fetch(cache.K, 0, seen, kKeyLanes, next);
-        for (int i = 0; i < my_turns; ++i) {
-            uint4 v[4];
+                for (int x = 0; x < 2 * kSteps; ++x) v[x] = keys[x];
+                if (i + 1 < my_units) fetch_keys(i + 1, seen, keys);
+                float z[2][4] = {};  // (two sums: half the chain)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = next[x];
-            if (i + 1 < my_turns) fetch(cache.K, i + 1, seen, kKeyLanes, next);
-            const int at = turn_begin(i) + lane / kKeyLanes;
-#pragma unroll
-            for (int x = 0; x < 4; x += kVecs) {
-                uint64_t k[4 * kVecs];
-#pragma unroll
-                for (int y = 0; y < kVecs; ++y) unpack_pairs(v[x + y], k + 4 * y);
-                float dot[GP];
-#pragma unroll
-                for (int g = 0; g < GP; ++g) {
-                    uint64_t sum = ptx::mul2(q[g][0], k[0]);
-#pragma unroll
-                    for (int e = 1; e < 4 * kVecs; ++e) sum = ptx::fma2(q[g][e], k[e], sum);
-                    float lo, hi;
-                    ptx::unpack2(sum, lo, hi);
-                    dot[g] = lo + hi;
+                for (int x = 0; x < kSteps; ++x) {
+                    multiply(z[0], v[2 * x].x, v[2 * x + 1].x, v[2 * x].y, v[2 * x + 1].y, q[x].x, q[x].y);
+                    multiply(z[1], v[2 * x].z, v[2 * x + 1].z, v[2 * x].w, v[2 * x + 1].w, q[x].z, q[x].w);
                 }
-                const int key = at + x / kVecs * (32 / kKeyLanes);
-                const float z = reduce_heads<GP, kKeyLanes>(dot, lane), s = key0 + key < seen ? z * c2 : __int_as_float(0xff800000);
-                top = fmaxf(top, s);
-                if (lane % kHeadLanes == 0) scores[key * GP + head] = s;
-            }
-        }
-        // the first values are on their way while the scores are turned into weights
-        if (my_turns > 0) fetch(cache.V, 0, seen, kRowLanes, next);
 #pragma unroll
-        for (int o = 16; o >= kKeyLanes; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (lane < kKeyLanes && lane % kHeadLanes == 0) of_warps[warp * GP + head] = top;
+                for (int y = 0; y < 4; ++y) {
+                    const int key = unit_begin(i) + r + (y >> 1) * 8, head = 2 * c + (y & 1);
+                    const float s = key0 + key < seen ? (z[0][y] + z[1][y]) * c2 : __int_as_float(0xff800000);
+                    top[y & 1] = fmaxf(top[y & 1], s);
+                    if (head < GP) scores[key * GP + head] = s;
+                }
+            }
+            // the first values are on their way while the scores are turned into weights
+            if (my_units > 0) fetch_values(0, 0, seen, values[0]);
+            if (my_units > 0) fetch_next(0, 0, 1, seen, values[1]);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int o = 16; o >= 4; o >>= 1) top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], o));
+                if (r == 0 && 2 * c + y < GP) of_warps[warp * GP + 2 * c + y] = top[y];
+            }
+        } else {
+            uint64_t q[GP][4 * kVecs];  // pairs of features
+#pragma unroll
+            for (int g = 0; g < GP; ++g)
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (g < shape.group)
+                        v = *reinterpret_cast<const uint4*>(Q + t * q_token + (h * shape.group + g) * q_head + (i * kKeyLanes + lane % kKeyLanes) * 8);
+                    unpack_pairs(v, q[g] + 4 * i);
+                }
+            // ---- scores, and their maximum ----
+            const int head = head_of<GP, kKeyLanes>(lane);
+            float top = -3.0e38f;
+            if (my_turns > 0) fetch(cache.K, 0, seen, kKeyLanes, next);
+            for (int i = 0; i < my_turns; ++i) {
+                uint4 v[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = next[x];
+                if (i + 1 < my_turns) fetch(cache.K, i + 1, seen, kKeyLanes, next);
+                const int at = turn_begin(i) + lane / kKeyLanes;
+#pragma unroll
+                for (int x = 0; x < 4; x += kVecs) {
+                    uint64_t k[4 * kVecs];
+#pragma unroll
+                    for (int y = 0; y < kVecs; ++y) unpack_pairs(v[x + y], k + 4 * y);
+                    float dot[GP];
+#pragma unroll
+                    for (int g = 0; g < GP; ++g) {
+                        uint64_t sum = ptx::mul2(q[g][0], k[0]);
+#pragma unroll
+                        for (int e = 1; e < 4 * kVecs; ++e) sum = ptx::fma2(q[g][e], k[e], sum);
+                        float lo, hi;
+                        ptx::unpack2(sum, lo, hi);
+                        dot[g] = lo + hi;
+                    }
+                    const int key = at + x / kVecs * (32 / kKeyLanes);
+                    const float z = reduce_heads<GP, kKeyLanes>(dot, lane), s = key0 + key < seen ? z * c2 : __int_as_float(0xff800000);
+                    top = fmaxf(top, s);
+                    if (lane % kHeadLanes == 0) scores[key * GP + head] = s;
+                }
+            }
+            // (as above)
+            if (my_turns > 0) fetch(cache.V, 0, seen, kRowLanes, next);
+#pragma unroll
+            for (int o = 16; o >= kKeyLanes; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            if (lane < kKeyLanes && lane % kHeadLanes == 0) of_warps[warp * GP + head] = top;
+        }
         __syncthreads();
         // ---- weights relative to this CTA's maxima, and their sums ----
         float m[GP], l[GP];
@@ -264,49 +355,91 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
             }
         }
         // ---- values ----
-        uint64_t o2[GP][4];
+        if constexpr (kTensor) {
+            // Rows 0 ... 7 of the first operand are the heads' weights rounded to bfloat16, rows 8 ... 15 what the rounding left over, rounded: the weights count
+            // with 16 bits, at no cost, as there are at most 8 heads.  Column n of product j is feature 8n + j, so that a lane's vectors are its columns.
+            // 64 features at a time (the sums of 128 and their vectors do not fit the registers).
+#pragma unroll 1
+            for (int y = 0; y < kHalves; ++y) {
+                float o[8][4] = {};
+                auto add = [&](int i, uint4 (&v)[4]) {
+                    uint32_t w[2], left[2];
 #pragma unroll
-        for (int g = 0; g < GP; ++g)
+                    for (int x = 0; x < 2; ++x) {
+                        const float* p = scores + (unit_begin(i) + c + 8 * x) * GP + r;
+                        const float w0 = r < GP ? p[0] : 0.0f, w1 = r < GP ? p[4 * GP] : 0.0f;
+                        w[x] = ptx::pack_bf16x2(w0, w1);
+                        left[x] = ptx::pack_bf16x2(w0 - __uint_as_float(w[x] << 16), w1 - __uint_as_float(w[x] & 0xffff0000u));
+                    }
+                    const uint32_t word[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w}, {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o2[g][e] = 0ull;
-        for (int i = 0; i < my_turns; ++i) {
-            uint4 v[4];
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t which = j & 1 ? 0x7632 : 0x5410;
+                        multiply(o[j], w[0], left[0], w[1], left[1], __byte_perm(word[0][j >> 1], word[1][j >> 1], which),
+                                 __byte_perm(word[2][j >> 1], word[3][j >> 1], which));
+                    }
+                };
+                for (int i = 0; i < my_units; ++i) {  // two of them are on their way, of this half or the next
+                    uint4 v[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = next[x];
-            if (i + 1 < my_turns) fetch(cache.V, i + 1, seen, kRowLanes, next);
-            const float* p = scores + (turn_begin(i) + lane / kRowLanes) * GP;
+                    for (int x = 0; x < 4; ++x) v[x] = values[0][x], values[0][x] = values[1][x];
+                    fetch_next(i, y, 2, seen, values[1]);
+                    add(i, v);
+                }
+                if (r < GP)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                uint64_t y[4];
-                unpack_pairs(v[x], y);
+                    for (int x = 0; x < 4; ++x) {  // columns 2c and 2c + 1
+                        float* dst = part + (warp * GP + r) * D + y * 64 + c * 16 + x * 4;
+                        const int j = x % 2 * 4, e = x / 2;
+                        *reinterpret_cast<float4*>(dst) = make_float4(o[j][e] + o[j][e + 2], o[j + 1][e] + o[j + 1][e + 2], o[j + 2][e] + o[j + 2][e + 2],
+                                                                      o[j + 3][e] + o[j + 3][e + 2]);
+                    }
+            }
+        } else {
+            uint64_t o2[GP][4];
 #pragma unroll
-                for (int g = 0; g < GP; ++g) {
-                    const float w = p[x * (32 / kRowLanes) * GP + g];
+            for (int g = 0; g < GP; ++g)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o2[g][e] = ptx::fma2(ptx::pack2(w, w), y[e], o2[g][e]);
+                for (int e = 0; e < 4; ++e) o2[g][e] = 0ull;
+            for (int i = 0; i < my_turns; ++i) {
+                uint4 v[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = next[x];
+                if (i + 1 < my_turns) fetch(cache.V, i + 1, seen, kRowLanes, next);
+                const float* p = scores + (turn_begin(i) + lane / kRowLanes) * GP;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    uint64_t y[4];
+                    unpack_pairs(v[x], y);
+#pragma unroll
+                    for (int g = 0; g < GP; ++g) {
+                        const float w = p[x * (32 / kRowLanes) * GP + g];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o2[g][e] = ptx::fma2(ptx::pack2(w, w), y[e], o2[g][e]);
+                    }
                 }
             }
+            float o[GP][8];
+#pragma unroll
+            for (int g = 0; g < GP; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (e % 2 == 0) ptx::unpack2(o2[g][e / 2], o[g][e], o[g][e + 1]);
+                }
+#pragma unroll
+            for (int g = 0; g < GP; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int x = 16; x >= kRowLanes; x >>= 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], x);
+            if (lane < kRowLanes)
+#pragma unroll
+                for (int g = 0; g < GP; ++g) {
+                    float4* dst = reinterpret_cast<float4*>(part + (warp * GP + g) * D + lane * 8);
+                    dst[0] = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
+                    dst[1] = make_float4(o[g][4], o[g][5], o[g][6], o[g][7]);
+                }
         }
-        float o[GP][8];
-#pragma unroll
-        for (int g = 0; g < GP; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e % 2 == 0) ptx::unpack2(o2[g][e / 2], o[g][e], o[g][e + 1]);
-            }
-#pragma unroll
-        for (int g = 0; g < GP; ++g)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int x = 16; x >= kRowLanes; x >>= 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], x);
-        if (lane < kRowLanes)
-#pragma unroll
-            for (int g = 0; g < GP; ++g) {
-                float4* dst = reinterpret_cast<float4*>(part + (warp * GP + g) * D + lane * 8);
-                dst[0] = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
-                dst[1] = make_float4(o[g][4], o[g][5], o[g][6], o[g][7]);
-            }
         __syncthreads();
         for (int i = tid; i < GP * D; i += kThreads) {
             float sum = 0.0f;

@@ -356,16 +356,17 @@ cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void
     return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, stream);
 }
 
-// Is it the faster one?  Its time goes by the bytes that a CTA reads, 27 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
-// other one's by the bytes in all, which it spreads evenly, after 12 us (blocks that are not cut) to 25 (cut ones, joined), and with weights 10 to 20
-// more.  The lengths are on the device: caches count as full.  us per call, few -> tensor cores, 32 heads on 8, d = 128: one token over 100 keys 6.9 / 12.6,
-// 1000 8.5 / 26.9, 4000 12.7 / 24.1, 16000 32.6 / 26.4, 4 over 4000 20.7 / 28.0, 16 over 1000 19.4 / 28.3, 16 tokens of one sequence over 500
-// 12.4 / 17.7, 8 each of four over 1000 32.9 / 28.0; 64 heads on 8, 8 tokens over 4000 69 / 44; 8 heads on 8 30 / 42.  With weights: 1 over 1000 10.3 / 36.4,
-// 16000 35 / 46, 32 over 4095 145 / 225, 64 heads on 8, 8 over 4000 81 / 75; four tokens of one sequence over 100 26.9 / 20.4.
+// Is it the faster one?  Its time goes by the bytes that a CTA reads, 25 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
+// other one's by the bytes in all, which it spreads evenly, after 12 us (blocks that are not cut) to 25 (cut ones, joined), and with weights 10 to 30
+// more.  The lengths are on the device: caches count as full.  us per call, few -> tensor cores, 32 heads on 8, d = 128: one token over 100 keys 6.9 / 13.1,
+// 1000 7.9 / 23.3, 4000 11.1 / 19.9, 16000 27.2 / 27.7, 16 over 1000 16.8 / 28.1, 8 over 4095 30.8 / 43.0, of all lengths up to that 27.6 / 28.7, 32 over 4095
+// 120 / 117, 16 tokens of one sequence over 500 10.5 / 17.4, 16 each of four over 3000 130 / 31; 64 heads on 8, 8 tokens over 4000 46 / 43; 8 heads on 8
+// 30 / 42.  With weights: 1 over 1000 9.9 / 32.6, 16000 31 / 47, 32 over 4095 134 / 223, 64 heads on 8, 8 over 4000 57 / 74; four tokens of one sequence
+// over 100 24.7 / 21.1.
 bool few_pays(const attnw_cache* c, const FewShape& f, int tokens, bool weigh) {
     if (weigh && tokens > c->sequences) return false;  // (a sequence's tokens take turns there)
-    long long most = f.gp <= 2 ? 1024 : f.gp == 4 ? 512 : 256;  // kB
-    if (weigh) most = f.gp <= 4 ? 4096 : 768;
+    long long most = f.gp <= 4 ? 1024 : 512;  // kB
+    if (weigh) most = f.gp <= 4 ? 16384 : 4096;
     if (tokens > c->sequences) most = most * 3 / 4;  // (the other one reads a sequence's keys once for all its tokens)
     return f.rounds * (f.max_keys * 4ll * c->d / 1024 + 128) <= most + 128;
 }
