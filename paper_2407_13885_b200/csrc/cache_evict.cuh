@@ -294,9 +294,9 @@ evict_move_kernel(paged::Cache cache, const int* table_out, int table_out_width,
             to[i] = -1;
             if (from[i] < 0 || (IN_PLACE && from[i] == t)) continue;
             const int page = paged::page_of(cache.table, cache, b, from[i]), page_to = target_page(t);
-            if (page < 0 || page_to < 0) continue;
+            if (page_to < 0) continue;
             to[i] = static_cast<long long>(paged::row_offset(cache, page_to, h, t) / 8 + piece);
-            v[i] = __ldcs(data + paged::row_offset(cache, page, h, from[i]) / 8 + piece);
+            v[i] = page >= 0 ? __ldcs(data + paged::row_offset(cache, page, h, from[i]) / 8 + piece) : make_uint4(0u, 0u, 0u, 0u);  // (reads as zeros)
         }
     };
     auto store = [&]() {
