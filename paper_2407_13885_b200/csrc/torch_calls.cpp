@@ -55,13 +55,10 @@ const at::Tensor* bf16_arg(PyObject* obj, const char* name, const at::Tensor* li
     return tensor_arg(obj, name, at::kBFloat16, "torch.bfloat16", like);
 }
 
-// The result: the caller's tensor `obj` (bfloat16, or also float32 where `f32_allowed`), or a new one where it is None.
-bool output_arg(PyObject* obj, const char* name, at::IntArrayRef shape, at::ScalarType new_type, bool f32_allowed, bool exact_type,
-                const char* shape_text, const at::Tensor& like, at::Tensor* out) {
-    if (obj == Py_None) {
-        *out = at::empty(shape, like.options().dtype(new_type).requires_grad(false));
-        return true;
-    }
+// The result: the caller's tensor `obj` (bfloat16, or also float32 where `f32_allowed`); none yet where it is None (new_on makes it).
+bool output_arg(PyObject* obj, const char* name, at::IntArrayRef shape, bool f32_allowed, bool exact_type, const char* shape_text,
+                const at::Tensor& like, at::Tensor* out) {
+    if (obj == Py_None) return true;
     const bool f32 = f32_allowed && THPVariable_Check(obj) && THPVariable_Unpack(obj).scalar_type() == at::kFloat;
     if (exact_type || f32 || (THPVariable_Check(obj) && THPVariable_Unpack(obj).scalar_type() == at::kBFloat16)) {
         const at::Tensor* t = tensor_arg(obj, name, f32 ? at::kFloat : at::kBFloat16, f32 ? "torch.float32" : "torch.bfloat16", &like);
@@ -86,6 +83,18 @@ bool stream_arg(PyObject* obj, void** out) {
     }
     *out = PyLong_AsVoidPtr(obj);
     return !PyErr_Occurred();
+}
+
+// New memory for a call on `stream`, which the device's current stream may use as well.  It comes from what belongs to that stream: a block of
+// the current one's may still be in use there by work in front, and would go to other work there as soon as the result is dropped.
+at::Tensor new_on(void* stream, at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like) {
+    const auto options = like.options().dtype(type).requires_grad(false);
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(like.device().index());
+    if (stream == static_cast<void*>(current.stream())) return at::empty(sizes, options);
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
+    at::Tensor t = at::empty(sizes, options);
+    t.record_stream(current);
+    return t;
 }
 
 bool float_arg(PyObject* obj, float* out) {
@@ -137,12 +146,11 @@ PyObject* py_attnw_fused(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if ((a[3] == Py_None && !is_float32(a[4], &f32)) || !float_arg(a[2], &scale)) return nullptr;
     const void *q_ptr = q->data_ptr(), *k_ptr = k->data_ptr();
     at::Tensor p;
-    if (!output_arg(a[3], "P", {B, H, N, N}, f32 ? at::kFloat : at::kBFloat16, true, false,
-                    "[B, H, N, N] in bfloat16 or float32", *q, &p))
-        return nullptr;
+    if (!output_arg(a[3], "P", {B, H, N, N}, true, false, "[B, H, N, N] in bfloat16 or float32", *q, &p)) return nullptr;
     const c10::cuda::CUDAGuard guard(q->device());
     void* stream;
     if (!stream_arg(a[5], &stream)) return nullptr;
+    if (!p.defined()) p = new_on(stream, {B, H, N, N}, f32 ? at::kFloat : at::kBFloat16, *q);
     const auto entry = p.scalar_type() == at::kBFloat16 ? attnw_fused : attnw_fused_f32;
     void* p_ptr = p.data_ptr();
     int rc;
@@ -170,10 +178,11 @@ PyObject* py_attn_fused(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void *q_ptr = q->data_ptr(), *k_ptr = k->data_ptr(), *v_ptr = v->data_ptr();
     const int B = static_cast<int>(q->size(0)), H = static_cast<int>(q->size(1)), N = static_cast<int>(q->size(2)), d = static_cast<int>(q->size(3));
     at::Tensor o;
-    if (!output_arg(a[4], "O", q->sizes(), at::kBFloat16, false, true, "[B, H, N, d]", *q, &o)) return nullptr;
+    if (!output_arg(a[4], "O", q->sizes(), false, true, "[B, H, N, d]", *q, &o)) return nullptr;
     const c10::cuda::CUDAGuard guard(q->device());
     void* stream;
     if (!stream_arg(a[5], &stream)) return nullptr;
+    if (!o.defined()) o = new_on(stream, q->sizes(), at::kBFloat16, *q);
     void* o_ptr = o.data_ptr();
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -198,12 +207,14 @@ PyObject* py_project_qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t B = x->size(0), N = x->size(1), d_model = x->size(2), H = wq->size(0), d = wq->size(1);
     const void *x_ptr = x->data_ptr(), *wq_ptr = wq->data_ptr(), *wk_ptr = wk->data_ptr();
     at::Tensor q, k;
-    if (!output_arg(a[3], "Q", {B, H, N, d}, at::kBFloat16, false, true, "[B, H, N, d]", *x, &q) ||
-        !output_arg(a[4], "K", {B, H, N, d}, at::kBFloat16, false, true, "[B, H, N, d]", *x, &k))
+    if (!output_arg(a[3], "Q", {B, H, N, d}, false, true, "[B, H, N, d]", *x, &q) ||
+        !output_arg(a[4], "K", {B, H, N, d}, false, true, "[B, H, N, d]", *x, &k))
         return nullptr;
     const c10::cuda::CUDAGuard guard(x->device());
     void* stream;
     if (!stream_arg(a[5], &stream)) return nullptr;
+    if (!q.defined()) q = new_on(stream, {B, H, N, d}, at::kBFloat16, *x);
+    if (!k.defined()) k = new_on(stream, {B, H, N, d}, at::kBFloat16, *x);
     void *q_ptr = q.data_ptr(), *k_ptr = k.data_ptr();
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -235,12 +246,11 @@ PyObject* py_softmax_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const long long rows = s->size(0), cols = s->size(1);
     const void* s_ptr = s->data_ptr();
     at::Tensor p;
-    if (!output_arg(a[1], "P", s->sizes(), f32 ? at::kFloat : at::kBFloat16, true, false,
-                    "[rows, cols] in bfloat16 or float32", *s, &p))
-        return nullptr;
+    if (!output_arg(a[1], "P", s->sizes(), true, false, "[rows, cols] in bfloat16 or float32", *s, &p)) return nullptr;
     const c10::cuda::CUDAGuard guard(s->device());
     void* stream;
     if (!stream_arg(a[3], &stream)) return nullptr;
+    if (!p.defined()) p = new_on(stream, s->sizes(), f32 ? at::kFloat : at::kBFloat16, *s);
     const auto entry = p.scalar_type() == at::kBFloat16 ? softmax_rows : softmax_rows_f32;
     void* p_ptr = p.data_ptr();
     int rc;
@@ -359,7 +369,7 @@ bool cache_arg(PyObject* const* a, attnw_cache* c, const at::Tensor** k_cache) {
     return true;
 }
 
-// Scratch memory of one call on `stream`: it belongs to that stream, so that whoever gets it next runs behind the call.
+// Scratch memory of one call on `stream`: it belongs to that stream alone, so that whoever gets it next runs behind the call.
 at::Tensor scratch(int64_t bytes, void* stream, const at::Tensor& like) {
     const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
     return at::empty({bytes}, like.options().dtype(at::kByte).requires_grad(false));
@@ -391,9 +401,7 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto* p_ptr = static_cast<const int*>(positions->data_ptr());
     const auto* f_ptr = static_cast<const double*>(frequencies->data_ptr());
     at::Tensor y;
-    if (a[6] == Py_None) {
-        y = at::empty(x->sizes(), x->options().requires_grad(false));
-    } else {
+    if (a[6] != Py_None) {
         const at::Tensor* t = strided_arg(a[6], "out", type, type_name, 4, x);
         if (!t) return nullptr;
         if (t->sizes() != x->sizes()) {
@@ -405,6 +413,7 @@ PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::cuda::CUDAGuard guard(x->device());
     void* stream;
     if (!stream_arg(a[7], &stream)) return nullptr;
+    if (!y.defined()) y = new_on(stream, x->sizes(), type, *x);
     const long long xs[3] = {x->stride(0), x->stride(1), x->stride(2)}, ys[3] = {y.stride(0), y.stride(1), y.stride(2)};
     const auto entry = f32 ? attnw_rope_f32 : attnw_rope;
     void* y_ptr = y.data_ptr();
@@ -460,9 +469,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto* p_ptr = positions ? static_cast<const int*>(positions->data_ptr()) : nullptr;
     const auto* f_ptr = frequencies ? static_cast<const double*>(frequencies->data_ptr()) : nullptr;
     at::Tensor out;
-    if (q && a[12] == Py_None) {
-        out = at::empty(q->sizes(), q->options().requires_grad(false));
-    } else if (q) {
+    if (q && a[12] != Py_None) {
         const at::Tensor* t = strided_arg(a[12], "Q_out", at::kBFloat16, "torch.bfloat16", 3, cache);
         if (!t) return nullptr;
         if (t->sizes() != q->sizes()) {
@@ -474,6 +481,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::cuda::CUDAGuard guard(cache->device());
     void* stream;
     if (!stream_arg(a[13], &stream)) return nullptr;
+    if (q && !out.defined()) out = new_on(stream, q->sizes(), at::kBFloat16, *q);
     const long long strides[8] = {q ? q->stride(0) : 0, q ? q->stride(1) : 0, k->stride(0), k->stride(1), v->stride(0), v->stride(1),
                                   q ? out.stride(0) : 0, q ? out.stride(1) : 0};
     void* o_ptr = q ? out.data_ptr() : nullptr;
@@ -515,10 +523,8 @@ PyObject* py_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* lse_ptr = lse ? static_cast<float*>(lse->data_ptr()) : nullptr;
     const float* mass_ptr = mass ? static_cast<const float*>(mass->data_ptr()) : nullptr;
     at::Tensor o, mass_out;
-    if (!output_arg(a[7], "O", q->sizes(), at::kBFloat16, false, true, "[tokens, heads, d]", *q, &o)) return nullptr;
-    if (mass && a[10] == Py_None) {
-        mass_out = at::empty(mass->sizes(), mass->options().requires_grad(false));
-    } else if (mass) {
+    if (!output_arg(a[7], "O", q->sizes(), false, true, "[tokens, heads, d]", *q, &o)) return nullptr;
+    if (mass && a[10] != Py_None) {
         const at::Tensor* t = f32_arg(a[10], "mass_out", {c.sequences, c.kv_heads, capacity}, cache);
         if (!t) return nullptr;
         mass_out = *t;
@@ -526,6 +532,8 @@ PyObject* py_attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::cuda::CUDAGuard guard(cache->device());
     void* stream;
     if (!stream_arg(a[11], &stream)) return nullptr;
+    if (!o.defined()) o = new_on(stream, q->sizes(), at::kBFloat16, *q);
+    if (mass && !mass_out.defined()) mass_out = new_on(stream, mass->sizes(), at::kFloat, *q);
     const long long strides[2] = {q->stride(0), q->stride(1)};
     const long long bytes = attn_paged_workspace(&c, static_cast<int>(tokens), static_cast<int>(heads), mass ? 1 : 0);
     at::Tensor workspace;
@@ -562,19 +570,18 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!small({width, capacity})) return nullptr;
     const float* mass_ptr = static_cast<const float*>(mass->data_ptr());
     const int* out_table = table_out ? static_cast<const int*>(table_out->data_ptr()) : nullptr;
-    const auto ints = cache->options().dtype(at::kInt).requires_grad(false);
     at::Tensor mass_out;
-    if (a[8] == Py_None) {
-        mass_out = at::empty({c.sequences, c.kv_heads, capacity}, mass->options().requires_grad(false));
-    } else {
+    if (a[8] != Py_None) {
         const at::Tensor* t = f32_arg(a[8], "mass_out", {c.sequences, c.kv_heads, capacity}, cache);
         if (!t) return nullptr;
         mass_out = *t;
     }
-    at::Tensor kept = at::empty({c.sequences, c.kv_heads, budget > 0 ? budget : 0}, ints), lengths_out = at::empty({c.sequences}, ints);
     const c10::cuda::CUDAGuard guard(cache->device());
     void* stream;
     if (!stream_arg(a[9], &stream)) return nullptr;
+    if (!mass_out.defined()) mass_out = new_on(stream, {c.sequences, c.kv_heads, capacity}, at::kFloat, *cache);
+    const at::Tensor kept = new_on(stream, {c.sequences, c.kv_heads, budget > 0 ? budget : 0}, at::kInt, *cache),
+                     lengths_out = new_on(stream, {c.sequences}, at::kInt, *cache);
     float* out_ptr = static_cast<float*>(mass_out.data_ptr());
     int *kept_ptr = static_cast<int*>(kept.data_ptr()), *length_ptr = static_cast<int*>(lengths_out.data_ptr());
     int rc;
@@ -582,7 +589,7 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     rc = attnw_cache_evict(&c, out_table, static_cast<int>(width), mass_ptr, out_ptr, kept_ptr, length_ptr, budget, recent, stream);
     Py_END_ALLOW_THREADS
     if (rc != ATTNW_OK) return failed(rc, "attnw_cache_evict");
-    PyObject *pk = THPVariable_Wrap(std::move(kept)), *pl = THPVariable_Wrap(std::move(lengths_out)), *pm = given_or_new(a[8], std::move(mass_out));
+    PyObject *pk = THPVariable_Wrap(kept), *pl = THPVariable_Wrap(lengths_out), *pm = given_or_new(a[8], std::move(mass_out));
     PyObject* all = pk && pl && pm ? PyTuple_Pack(3, pk, pl, pm) : nullptr;
     Py_XDECREF(pk);
     Py_XDECREF(pl);
