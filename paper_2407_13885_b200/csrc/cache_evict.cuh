@@ -257,6 +257,10 @@ evict_select_kernel(paged::Cache cache, const float* mass, float* mass_out, int*
     for (int t = left + tid; t < capacity_out; t += kSelectThreads) out[t] = 0.0f;
 }
 
+// The place that key t comes from, by what evict_select wrote; -1: none that the sequence has (the two kernels are two launches, and what lies
+// between them is the caller's memory: a place out of it is looked up in the table only where the table has it).
+__host__ __device__ __forceinline__ int source_of(int kept, int t, int length) { return kept >= t && kept < length ? kept : -1; }
+
 constexpr int kMoveThreads = 256;
 constexpr int kFlight = 8;  // 16-byte pieces of a thread in flight
 
@@ -268,7 +272,7 @@ evict_move_kernel(paged::Cache cache, const int* table_out, int table_out_width,
     const int pieces = cache.d / 8 / slices;  // of a key, this CTA's: a power of two
     const int slice = static_cast<int>(blockIdx.x) % slices;
     const int row = static_cast<int>(blockIdx.y), b = row / cache.kv_heads, h = row % cache.kv_heads;
-    const int left = min(paged::length_of(cache, b), budget);
+    const int length = paged::length_of(cache, b), left = min(length, budget);
     const int* keep = kept + static_cast<size_t>(row) * budget;
     uint4* data = reinterpret_cast<uint4*>(blockIdx.z == 0 ? cache.K : cache.V);
     const int keys = kMoveThreads * kFlight / pieces;  // of a step
@@ -286,7 +290,7 @@ evict_move_kernel(paged::Cache cache, const int* table_out, int table_out_width,
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int t = t0 + first + i * stride;
-            from[i] = t < left ? keep[t] : -1;
+            from[i] = t < left ? source_of(keep[t], t, length) : -1;
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
