@@ -123,6 +123,8 @@ struct Tiles {
             parity ^= 1u;
         }
     }
+    // Is tile `it` of `loads` of this kind the last that its stage has had?  (Only that one's arrival can be told by the stage's parity.)
+    __host__ __device__ __forceinline__ bool last_of_stage(int it, int loads) const { return it + (behind - first) >= loads; }
 };
 
 struct Barriers {
@@ -733,7 +735,7 @@ attn_onepass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int kind = 0; kind < 2; ++kind) {
                 Ring tile(kind);
                 for (int it = 0; it < loads[kind]; ++it, tile.next())
-                    while (it + kStages >= loads[kind] && !ptx::mbar_try_wait(&bars->k_full[tile.stage], tile.parity) && clock64() - t0 < kWaitLimitCycles / 8) {
+                    while (tile.last_of_stage(it, loads[kind]) && !ptx::mbar_try_wait(&bars->k_full[tile.stage], tile.parity) && clock64() - t0 < kWaitLimitCycles / 8) {
                     }
             }
             while (!ptx::mbar_try_wait(&bars->q_full, 0) && clock64() - t0 < kWaitLimitCycles / 8) {
