@@ -194,7 +194,8 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
  *   workspace    device, 16-byte aligned, at least attn_paged_workspace(cache, tokens, heads, mass != NULL) bytes, in use until the
  *                call's work has ended; it keeps nothing from one call to the next and may hold anything
  *   heads        a multiple of kv_heads, at most 128 to one;  scale finite, >= 0;  tokens * heads < 2^29
- * Keys behind a sequence's length are never part of a result, whatever the cache holds there.
+ * Keys that a token does not see are never part of its result, whatever the cache holds there: those behind its own place, and those behind the sequence's
+ * length.  A value that is not finite makes its feature of the tokens that see it, and of no others, not finite.
  */
 int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
                float* mass_out, void* workspace, long long workspace_bytes, int tokens, int heads, float scale, void* stream);

@@ -1,4 +1,6 @@
 """The paged cache on the GPU where tables, values or sizes are out of the ordinary."""
+import math
+
 import pytest
 import torch
 
@@ -12,6 +14,13 @@ def attnw():
     from paper_2407_13885_b200 import binding
     yield binding
     assert binding.query_status() == 0
+
+
+@pytest.fixture(params=["tensor_cores", "few"])
+def variant(attnw, request):
+    attnw.set_paged_variant(request.param)
+    yield request.param
+    attnw.set_paged_variant("auto")
 
 
 def bits(x):
@@ -51,3 +60,55 @@ def test_eviction_of_keys_without_a_page(attnw, in_place, d):
                 want_V[target, h, t % page] = V0[source, h, s % page] if there else 0.0
     assert zeros >= 16
     assert torch.equal(bits(c.K), bits(want_K)) and torch.equal(bits(c.V), bits(want_V))
+
+
+# ---- values that are not finite -----------------------------------------------------------------------------------------------
+
+def attend(attnw, c, Q, scale=0.125):
+    lse = torch.full(Q.shape[:2], 7.0, device="cuda")
+    mass = torch.rand(len(c.pairs), c.Hkv, c.width * c.page, generator=torch.Generator().manual_seed(3)).cuda()
+    O, out = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, scale, lse=lse, mass=mass)
+    torch.cuda.synchronize()
+    assert attnw.query_status() == 0
+    return O, lse, out, mass
+
+
+def put(c, cache, b, at, h, feature, value):
+    cache[int(c.table[b, at // c.page]), h, at % c.page, feature] = value
+
+
+VALUES = [  # (H, Hkv, d, page, pairs, [(sequence, key, key head, features, value)])
+    (8, 2, 64, 16, [(40, 300), (200, 700), (5, 5), (1, 130)],
+     [(0, 280, 0, [3], math.nan), (1, 650, 1, [0, 5, 63], math.inf), (1, 699, 0, [10], -math.inf), (2, 4, 0, list(range(64)), math.nan),
+      (1, 600, 0, [20], math.inf), (1, 620, 0, [20], -math.inf), (1, 50, 1, [7], math.inf), (3, 129, 1, [1], math.nan)]),
+    (4, 4, 128, 64, [(300, 300), (7, 1000)],
+     [(0, 0, 0, [0], math.nan), (0, 127, 1, [64, 65, 127], math.inf), (0, 128, 2, [1, 90], math.nan), (0, 299, 3, [17], -math.inf), (0, 255, 3, [17, 18], math.nan),
+      (1, 999, 0, list(range(128)), math.nan), (1, 994, 1, [5], math.inf)]),
+    (6, 2, 128, 32, [(130, 3000)], [(0, 2870, 0, [2], math.nan), (0, 2999, 1, [33, 100], math.inf), (0, 2944, 1, [34], math.nan), (0, 12, 0, [50], math.nan)]),
+    (3, 1, 64, 16, [(90, 80)], [(0, 79, 0, [8], math.nan), (0, 0, 0, [9], math.inf)]),
+]
+
+
+@pytest.mark.parametrize("H,Hkv,d,page,pairs,places", VALUES)
+def test_values_that_are_not_finite_reach_only_the_tokens_that_see_them(attnw, variant, H, Hkv, d, page, pairs, places):
+    c = Paged(pairs, Hkv, d, page, seed=21, front=1, behind=1)
+    Q = c.normal(c.tokens, H, d)
+    clean = attend(attnw, c, Q)
+    starts = c.starts.tolist()
+    hit = torch.zeros(c.tokens, H, d, dtype=torch.bool)
+    G = H // Hkv
+    for b, at, h, features, value in places:
+        put(c, c.V, b, at, h, torch.tensor(features), value)
+        n, length = pairs[b]
+        first = max(0, at - (length - n))    # the first token that sees the key
+        for f in features:
+            hit[starts[b] + first:starts[b + 1], h * G:(h + 1) * G, f] = True
+    for _ in range(3):
+        O, lse, out, _ = attend(attnw, c, Q)
+        first, last = starts[0], starts[-1]
+        bad = ~torch.isfinite(O.float().cpu())[first:last]
+        assert torch.equal(bad, hit[first:last])
+        # rows and features have nothing to do with one another: the others are the same to the last bit
+        keep = ~hit[first:last]
+        assert torch.equal(O.cpu()[first:last][keep], clean[0].cpu()[first:last][keep])
+        assert torch.equal(lse.cpu()[first:last], clean[1].cpu()[first:last]) and torch.equal(out, clean[2])
