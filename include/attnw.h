@@ -195,7 +195,8 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
  *                call's work has ended; it keeps nothing from one call to the next and may hold anything
  *   heads        a multiple of kv_heads, at most 128 to one;  scale finite, >= 0;  tokens * heads < 2^29
  * Keys that a token does not see are never part of its result, whatever the cache holds there: those behind its own place, and those behind the sequence's
- * length.  A value that is not finite makes its feature of the tokens that see it, and of no others, not finite.
+ * length.  A value that is not finite makes its feature of the tokens that see it, and of no others, not finite.  A score that is not a number makes its
+ * row's O and lse, and the weights that it adds to, not a number.
  */
 int attn_paged(const attnw_cache* cache, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
                float* mass_out, void* workspace, long long workspace_bytes, int tokens, int heads, float scale, void* stream);

@@ -459,7 +459,7 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
         for (int i = 2 * (rank * kThreads + tid); i < shape.group * D; i += 2 * S * kThreads) {
             const int g = i / D;
             float sum;
-            const float M = factors(g, &sum), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const float M = factors(g, &sum), inv = sum != 0.0f ? 1.0f / sum : 0.0f;  // (not a number where a score was none)
             float a = 0.0f, b2 = 0.0f;
             for (int c = 0; c < S; ++c) {
                 const float f = ptx::ex2_approx(stats[c * GP + g].x - M) * inv;
@@ -480,7 +480,7 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
             float sum;
             const float M = factors(tid, &sum);
             lse[static_cast<size_t>(t) * shape.heads + h * shape.group + tid] =
-                sum > 0.0f ? 0.69314718055994531f * (M + ptx::lg2_approx(sum)) : __int_as_float(0xff800000);
+                sum != 0.0f ? 0.69314718055994531f * (M + ptx::lg2_approx(sum)) : __int_as_float(0xff800000);
         }
         if (WEIGH) {
             float f[GP];
@@ -488,12 +488,14 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
             for (int g = 0; g < GP; ++g) {
                 float sum;
                 const float M = factors(g, &sum);
-                f[g] = sum > 0.0f && g < shape.group ? ptx::ex2_approx(stats[rank * GP + g].x - M) / sum : 0.0f;
+                f[g] = sum != 0.0f ? ptx::ex2_approx(stats[rank * GP + g].x - M) / sum : 0.0f;
             }
-            for (int i = tid; i < (unit1 - unit0) * kUnit; i += kThreads) {
+            // (only what is a weight: a head of the group, of a key that the token sees)
+            for (int i = tid; i < (unit1 - unit0) * kUnit && key0 + i < seen; i += kThreads) {
                 float w = 0.0f;
 #pragma unroll
-                for (int g = 0; g < GP; ++g) w = fmaf(scores[i * GP + g], f[g], w);
+                for (int g = 0; g < GP; ++g)
+                    if (g < shape.group) w = fmaf(scores[i * GP + g], f[g], w);
                 weights[i] += w;
             }
         }

@@ -379,10 +379,11 @@ __device__ __noinline__ void lose_features(const int* first_key, int col0, int c
         if (first_key[c] < seen) dst[c] = T(__int_as_float(0x7fc00000));
 }
 
-// The logarithm of a row's sum l 2^top: to the caller, and for mass_kernel.
+// The logarithm of a row's sum l 2^top: to the caller, and for mass_kernel.  (A sum is zero, where the row sees nothing, or positive, or not a number, where a
+// score was none: nowhere may the last be taken for the first.)
 __device__ __forceinline__ void store_lse(const paged::Cache& c, const Shape& s, float* lse, float* lse2, size_t out_row, long long q_tile, int h, int row, float top,
                                           float l) {
-    const float log2_sum = l > 0.0f ? top + ptx::lg2_approx(l) : __int_as_float(0xff800000);
+    const float log2_sum = l != 0.0f ? top + ptx::lg2_approx(l) : __int_as_float(0xff800000);
     if (lse) lse[out_row] = 0.69314718055994531f * log2_sum;
     if (lse2 && q_tile < s.q_tiles) lse2[lse2_row(c, q_tile, h) + row] = -log2_sum;  // (the host's bound holds for tokens of one sequence each)
 }
@@ -937,15 +938,15 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     if (!whole) {
                         const float l_other = other_steps > 0 ? peer[0] + peer[kTile] : 0.0f, mb_other = other_steps > 0 ? peer[2 * kTile] : mb;
                         // (a unit that has seen nothing of the row has a sum of zero, and its offset no say)
-                        top = l_own > 0.0f ? (l_other > 0.0f ? fmaxf(mb, mb_other) : mb) : mb_other;
-                        f_own = l_own > 0.0f ? ptx::ex2_approx(mb - top) : 0.0f;
-                        f_other = l_other > 0.0f ? ptx::ex2_approx(mb_other - top) : 0.0f;
+                        top = l_own != 0.0f ? (l_other != 0.0f ? fmaxf(mb, mb_other) : mb) : mb_other;
+                        f_own = l_own != 0.0f ? ptx::ex2_approx(mb - top) : 0.0f;
+                        f_other = l_other != 0.0f ? ptx::ex2_approx(mb_other - top) : 0.0f;
                         l_row = l_own * f_own + l_other * f_other;
                     }
                 }
                 const bool joined = seg.part >= 0;  // by combine_kernel
                 if (!joined) {
-                    const float inv = l_row > 0.0f ? 1.0f / l_row : 0.0f;
+                    const float inv = l_row != 0.0f ? 1.0f / l_row : 0.0f;
                     f_own *= inv;
                     f_other *= inv;
                 }
@@ -1063,9 +1064,9 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
     const int rows = x.tokens * shape.group;
     // A part's offset and sum, and this lane's columns of its O, into what a row has so far.
     auto add = [](float2 st, const float (&o)[kCols], float& top, float& l, float (&v)[kCols]) {
-        if (!(st.y > 0.0f)) return;
-        const float next = l > 0.0f ? fmaxf(top, st.x) : st.x;
-        const float f_before = l > 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(st.x - next);
+        if (st.y == 0.0f) return;
+        const float next = l != 0.0f ? fmaxf(top, st.x) : st.x;
+        const float f_before = l != 0.0f ? ptx::ex2_approx(top - next) : 0.0f, f_new = ptx::ex2_approx(st.x - next);
         top = next;
         l = l * f_before + st.y * f_new;
 #pragma unroll
@@ -1084,7 +1085,7 @@ combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant
     auto store = [&](int r, float top, float l, const float (&v)[kCols]) {
         const int token = r / shape.group, g = r - token * shape.group;
         const size_t out_row = static_cast<size_t>(x.token0 + token) * shape.heads + x.h * shape.group + g;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
         __nv_bfloat16* dst = O + out_row * D + lane * kCols;
 #pragma unroll
         for (int c = 0; c < kCols; c += 2) *reinterpret_cast<uint32_t*>(dst + c) = ptx::pack_bf16x2(v[c] * inv, v[c + 1] * inv);

@@ -112,3 +112,50 @@ def test_values_that_are_not_finite_reach_only_the_tokens_that_see_them(attnw, v
         keep = ~hit[first:last]
         assert torch.equal(O.cpu()[first:last][keep], clean[0].cpu()[first:last][keep])
         assert torch.equal(lse.cpu()[first:last], clean[1].cpu()[first:last]) and torch.equal(out, clean[2])
+
+
+@pytest.mark.parametrize("H,Hkv,d,page", [(8, 2, 64, 16), (6, 2, 128, 64), (2, 2, 128, 32), (3, 3, 64, 16)])
+def test_scores_that_are_not_numbers(attnw, variant, H, Hkv, d, page):
+    # A score of NaN makes its row's sum NaN, and with it the row's result, its logarithm and all of its weights.
+    pairs = [(1, 9000), (70, 500), (3, 300), (2, 40), (1, 64), (1, 9100)]
+    if variant == "few":
+        pairs[1] = (9, 500)
+    c = Paged(pairs, Hkv, d, page, seed=22)
+    Q = c.normal(c.tokens, H, d)
+    clean = attend(attnw, c, Q)
+    starts = c.starts.tolist()
+    rows = torch.zeros(c.tokens, H, dtype=torch.bool)
+    keys = torch.zeros(len(pairs), Hkv, c.width * page, dtype=torch.bool)
+    G = H // Hkv
+    n1 = pairs[1][0]
+    for b, at, h in ((0, 4321, 0), (1, 500 - n1 + 4, 1), (5, 0, 1), (5, 9099, 0)):
+        put(c, c.K, b, at, h, torch.tensor([5]), math.nan)
+        n, length = pairs[b]
+        rows[starts[b] + max(0, at - (length - n)):starts[b + 1], h * G:(h + 1) * G] = True
+        keys[b, h, :length] = True
+    Q[starts[2], 0, 3] = math.nan              # the first of three tokens: the last two keys are not its
+    rows[starts[2], 0] = True
+    keys[2, 0, :298] = True
+    O, lse, out, prior = attend(attnw, c, Q)
+    assert torch.equal(torch.isnan(O.float()).cpu(), rows[..., None].expand(-1, -1, d))
+    assert torch.equal(torch.isnan(lse).cpu(), rows) and torch.equal(torch.isnan(out).cpu(), keys)
+    assert torch.equal(O.cpu()[~rows], clean[0].cpu()[~rows]) and torch.equal(lse.cpu()[~rows], clean[1].cpu()[~rows])
+    untouched = ~keys
+    untouched[2, 0, 298:300] = False           # (two of three tokens: the same sums, but checked apart)
+    assert torch.equal(out.cpu()[untouched], clean[2].cpu()[untouched])
+    assert float((out[2, 0, 298:300] - clean[2][2, 0, 298:300]).abs().max()) <= 2.0 ** -22 * 8
+
+
+def test_a_score_of_minus_infinity_weighs_nothing(attnw, variant):
+    # Groups of three heads: what fills the group up has no say, also where its score of 0 times infinity is NaN.
+    c = Paged([(1, 400), (2, 90)], 2, 64, 16, seed=23)
+    Q = c.normal(c.tokens, 6, 64)
+    Q[..., 0] = Q[..., 0].abs() + 0.5
+    for b, at in ((0, 17), (1, 60)):
+        put(c, c.K, b, at, slice(None), torch.tensor([0]), -1e30)
+    want = attend(attnw, c, Q)
+    for b, at in ((0, 17), (1, 60)):
+        put(c, c.K, b, at, slice(None), torch.tensor([0]), -math.inf)
+    got = attend(attnw, c, Q)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
