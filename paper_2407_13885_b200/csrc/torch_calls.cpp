@@ -580,7 +580,8 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* stream;
     if (!stream_arg(a[9], &stream)) return nullptr;
     if (!mass_out.defined()) mass_out = new_on(stream, {c.sequences, c.kv_heads, capacity}, at::kFloat, *cache);
-    const at::Tensor kept = new_on(stream, {c.sequences, c.kv_heads, budget > 0 ? budget : 0}, at::kInt, *cache),
+    // (a budget that the call refuses, below 1 or more than the pages hold, gets no memory of its size)
+    const at::Tensor kept = new_on(stream, {c.sequences, c.kv_heads, budget > 0 && budget <= capacity ? budget : 1}, at::kInt, *cache),
                      lengths_out = new_on(stream, {c.sequences}, at::kInt, *cache);
     float* out_ptr = static_cast<float*>(mass_out.data_ptr());
     int *kept_ptr = static_cast<int*>(kept.data_ptr()), *length_ptr = static_cast<int*>(lengths_out.data_ptr());

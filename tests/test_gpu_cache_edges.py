@@ -62,6 +62,22 @@ def test_eviction_of_keys_without_a_page(attnw, in_place, d):
     assert torch.equal(bits(c.K), bits(want_K)) and torch.equal(bits(c.V), bits(want_V))
 
 
+def test_a_budget_that_is_refused_takes_no_memory(attnw):
+    c = Paged([(0, 100)] * 3, 2, 64, 16)
+    mass = torch.rand(3, 2, c.width * 16, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for budget in (c.width * 16 + 1, 10 ** 6, 2 ** 31 - 1, 0, -1, -2 ** 31):   # (2^31 - 1: 51 GB of places)
+        with pytest.raises(attnw.AttnwError) as e:
+            attnw.cache_evict(c.K, c.V, c.table, c.lengths, mass, budget, 0)
+        assert e.value.code == 2
+    assert torch.cuda.max_memory_allocated() - before < 1 << 20
+    for budget, recent in ((2 ** 31, 0), (8, 2 ** 31), (-2 ** 31 - 1, 0)):
+        with pytest.raises(ValueError):
+            attnw.cache_evict(c.K, c.V, c.table, c.lengths, mass, budget, recent)
+
+
 # ---- values that are not finite -----------------------------------------------------------------------------------------------
 
 def attend(attnw, c, Q, scale=0.125):
