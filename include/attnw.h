@@ -131,7 +131,7 @@ int attnw_project_qk(const void* X, const void* Wq, const void* Wk, void* Q, voi
  *
  *   X, Y         device, bfloat16 (attnw_rope) or float32 (attnw_rope_f32), [B, H, N, d] with the strides given: x_strides[3], y_strides[3], HOST
  *                arrays, in elements, of the first three dimensions; rows of d are contiguous and begin on 16-byte boundaries.  Y may be X with the
- *                same strides (in place); any other overlap is refused.  A dimension of X may be broadcast (stride 0), none of Y.
+ *                same strides (in place); any other overlap is refused.  A dimension of X may be broadcast (stride 0); the rows of Y must not lie on one another.
  *   positions    device, int32, [B, N]; any value
  *   frequencies  device, float64, [rotary / 2], radians a position; may be NULL where rotary is 0
  *   B,H,N        >= 1, H <= 65535;  d in {64, 128};  rotary a multiple of 16 (else ATTNW_ERR_UNSUPPORTED), 0 ... d

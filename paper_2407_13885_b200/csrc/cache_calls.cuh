@@ -12,14 +12,16 @@ struct Extent {
     unsigned long long inner = 0;  // bytes that the rows of one token, or of tokens whole pitches apart, cover of a pitch
 };
 
-// Strides of a kernel's operand: not negative, and rows on 16-byte boundaries.  No dimension with more than one index may be
-// broadcast where `written`.  Returns an attnw_status.
-int check_strides(const long long* strides, const long long* sizes, int n, int esize, bool written) {
+// Strides of a kernel's operand: not negative, and rows on 16-byte boundaries.  `least`: of a dimension with more than one index, in elements; 0 where it
+// may be broadcast, the length of a row where rows are written, which then must not lie on one another (nor along two dimensions alike).  Returns an attnw_status.
+int check_strides(const long long* strides, const long long* sizes, int n, int esize, long long least) {
     for (int i = 0; i < n; ++i) {
         if (sizes[i] <= 1) continue;
         if (strides[i] < 0 || strides[i] > (1ll << 47) / (sizes[i] - 1)) return ATTNW_ERR_BAD_SHAPE;  // (an array lies within 2^48 elements)
         if (strides[i] * esize % 16 != 0) return ATTNW_ERR_MISALIGNED;
-        if (written && strides[i] == 0) return ATTNW_ERR_BAD_SHAPE;
+        if (strides[i] < least) return ATTNW_ERR_BAD_SHAPE;
+        for (int j = 0; j < i; ++j)
+            if (least > 1 && sizes[j] > 1 && strides[j] == strides[i]) return ATTNW_ERR_BAD_SHAPE;
     }
     return ATTNW_OK;
 }
@@ -77,8 +79,8 @@ int rope_entry(const void* X, const int* positions, const double* frequencies, v
     int rc = check_turn(frequencies, rotary, d, layout, amplitude);
     if (rc != ATTNW_OK) return rc;
     const long long sizes[3] = {B, H, N};
-    rc = check_strides(x_strides, sizes, 3, sizeof(T), false);
-    if (rc == ATTNW_OK) rc = check_strides(y_strides, sizes, 3, sizeof(T), true);
+    rc = check_strides(x_strides, sizes, 3, sizeof(T), 0);
+    if (rc == ATTNW_OK) rc = check_strides(y_strides, sizes, 3, sizeof(T), d);
     if (rc != ATTNW_OK) return rc;
     if (!aligned16(X) || !aligned16(Y) || !aligned4(positions)) return ATTNW_ERR_MISALIGNED;
     const Extent x = extent_of(X, x_strides, sizes, 3, 2, d, sizeof(T)), y = extent_of(Y, y_strides, sizes, 3, 2, d, sizeof(T));
@@ -147,10 +149,10 @@ int append_entry(const attnw_cache* c, const void* Q, const void* K, const void*
     rc = check_turn(frequencies, rotary, c->d, layout, amplitude);
     if (rc != ATTNW_OK) return rc;
     const long long q_sizes[2] = {tokens, Q ? heads : 1}, kv_sizes[2] = {tokens, c->kv_heads};
-    rc = check_strides(strides + 2, kv_sizes, 2, 2, false);
-    if (rc == ATTNW_OK) rc = check_strides(strides + 4, kv_sizes, 2, 2, false);
-    if (rc == ATTNW_OK && Q) rc = check_strides(strides, q_sizes, 2, 2, false);
-    if (rc == ATTNW_OK && Q) rc = check_strides(strides + 6, q_sizes, 2, 2, true);
+    rc = check_strides(strides + 2, kv_sizes, 2, 2, 0);
+    if (rc == ATTNW_OK) rc = check_strides(strides + 4, kv_sizes, 2, 2, 0);
+    if (rc == ATTNW_OK && Q) rc = check_strides(strides, q_sizes, 2, 2, 0);
+    if (rc == ATTNW_OK && Q) rc = check_strides(strides + 6, q_sizes, 2, 2, c->d);
     if (rc != ATTNW_OK) return rc;
     if (!aligned16(K) || !aligned16(V) || !aligned16(Q) || !aligned16(Q_out) || !aligned4(starts) || !aligned4(positions)) return ATTNW_ERR_MISALIGNED;
     const Extent k = extent_of(K, strides + 2, kv_sizes, 2, 0, c->d, 2), v = extent_of(V, strides + 4, kv_sizes, 2, 0, c->d, 2);
@@ -381,7 +383,7 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     if (heads / c->kv_heads > 128) return ATTNW_ERR_UNSUPPORTED;
     if (static_cast<long long>(tokens) * heads > INT_MAX / 4) return ATTNW_ERR_BAD_SHAPE;
     const long long sizes[2] = {tokens, heads};
-    rc = check_strides(q_strides, sizes, 2, 2, true);  // (a tensor map has no broadcast dimensions, and strides below 2^40 bytes)
+    rc = check_strides(q_strides, sizes, 2, 2, 1);  // (a tensor map has no broadcast dimensions, and strides below 2^40 bytes)
     if (rc != ATTNW_OK) return rc;
     if ((tokens > 1 && q_strides[0] >= 1ll << 39) || (heads > 1 && q_strides[1] * (heads / c->kv_heads) >= 1ll << 39)) return ATTNW_ERR_BAD_SHAPE;
     if (!aligned16(Q) || !aligned16(O) || !aligned4(starts) || !aligned4(lse) || !aligned4(mass) || !aligned4(mass_out)) return ATTNW_ERR_MISALIGNED;
