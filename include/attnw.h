@@ -204,7 +204,8 @@ long long attn_paged_workspace(const attnw_cache* cache, int tokens, int heads, 
 
 /*
  * Which kernel attn_paged uses (process-wide; the results agree within the roundings):
- *   0  by size (default): 2 where the caches, were they full, would hold few keys in all (decoding steps of short or middling sequences), else 1
+ *   0  by size (default): 2 where the caches, were they full, would hold few keys in all (decoding steps of short or middling sequences), else 1; with mass
+ *      and more than 16 tokens 2 for the sequences with at most 8 of them and 1, in the same call, for those with more
  *   1  tensor cores: one CTA an SM, all blocks of queries cut into equal stretches; weights of keys by a second kernel
  *   2  few tokens: one cluster of CTAs a (token, key head), or with mass a (sequence, key head), in one launch; it has no waits and
  *      ignores the status word (attnw_query_status).  ATTNW_ERR_UNSUPPORTED for more than 8 query heads a key head, or caches whose scores

@@ -33,6 +33,7 @@ struct Shape {
     int tokens, heads, group;
     int cluster;    // CTAs of an item
     int max_keys;   // that a CTA may have, a multiple of kUnit
+    int turns;      // with weights: tokens of a sequence, at most; those with more are attn_paged_kernel's
 };
 
 template <int D, int GP>
@@ -138,6 +139,7 @@ attn_few_kernel(const __nv_bfloat16* Q, long long q_token, long long q_head, con
         length = paged::length_of(cache, b);
         t0 = min(max(s0, 0), shape.tokens);
         t1 = min(max(end, 0), shape.tokens);
+        if (t1 - t0 > shape.turns) return;  // (all CTAs of the cluster)
     } else {
         t0 = item / cache.kv_heads;
         t1 = t0 + 1;

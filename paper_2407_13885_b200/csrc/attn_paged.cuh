@@ -126,6 +126,7 @@ struct Shape {
     int part_rows;             // rows of a slot of the workspace; 0: no block can be cut
     int q_tiles;               // query tiles a key head, at most (of all sequences)
     int ctas;                  // of attn_paged_kernel
+    int least;                 // sequences with fewer new tokens are attn_few_kernel's; 1: none are
 };
 
 // A sequence's blocks.
@@ -153,12 +154,23 @@ __device__ __forceinline__ Share share_of(const paged::Cache& c, const Shape& s,
     const int s0 = starts[b], s1 = starts[b + 1];
     const int t0 = min(max(s0, 0), s.tokens), t1 = min(max(s1, 0), s.tokens);
     r.n = max(t1 - t0, 0);
+    if (r.n < s.least) r.n = 0;
     r.token0 = t0;
     r.length = paged::length_of(c, b);
     const long long seen = static_cast<long long>(r.length) - (static_cast<long long>(s1) - t0) + 1;
     r.seen0 = static_cast<int>(min(max(seen, -(1ll << 30)), 1ll << 30));
     r.blocks = (r.n + 2 * s.tile_tokens - 1) / (2 * s.tile_tokens);
     return r;
+}
+
+// Are all sequences attn_few_kernel's (Shape::least)?  By all threads of a block, in front of everything else: then the launch has nothing to do, and what
+// it would set up takes longer than to find that out.
+__device__ __forceinline__ bool nothing_to_do(const paged::Cache& c, const Shape& s, const int* starts) {
+    ptx::grid_dependency_wait();
+    bool some = false;
+    for (int b = static_cast<int>(threadIdx.x); b < c.sequences; b += static_cast<int>(blockDim.x))
+        some = some || static_cast<long long>(starts[b + 1]) - starts[b] >= s.least;  // (no fewer than are within the tokens)
+    return __syncthreads_or(some) == 0;
 }
 
 __device__ __forceinline__ long long warp_sum(long long x) {
@@ -388,7 +400,9 @@ __device__ __forceinline__ void store_lse(const paged::Cache& c, const Shape& s,
     if (lse2 && q_tile < s.q_tiles) lse2[lse2_row(c, q_tile, h) + row] = -log2_sum;  // (the host's bound holds for tokens of one sequence each)
 }
 
-template <int D>
+// APART: the kernel for few tokens has the other sequences (Shape::least > 1).  A form of its own, since the question at the beginning, asked at run time by all
+// calls, cost 2 % (4 x 2048 tokens over some 6000 keys 705 -> 722 us).
+template <int D, bool APART>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, float scale_log2e,
@@ -402,6 +416,9 @@ attn_paged_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
+    if constexpr (APART) {
+        if (nothing_to_do(cache, shape, starts)) return;
+    }
 
     // ---- set-up ------------------------------------------------------------------------------
     if (warp == kProducer && lane == 0) {
@@ -1047,12 +1064,13 @@ constexpr int kJoinRows = 4;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32)
-combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const float* part_o, const float2* part_stats, const Join* joins,
-               __nv_bfloat16* O, float* lse, float* lse2) {
+combine_kernel(const __grid_constant__ paged::Cache cache, const __grid_constant__ Shape shape, const int* starts, const float* part_o, const float2* part_stats,
+               const Join* joins, __nv_bfloat16* O, float* lse, float* lse2) {
     constexpr int kCols = D / 32;
     __shared__ uint8_t slot_of[256];  // of each part: 0, 1; 2: the CTA has none of the block
     __shared__ float sums[kJoinWarps][32 * kCols + 2];
     ptx::grid_dependency_wait();
+    if (shape.least > 1 && nothing_to_do(cache, shape, starts)) return;  // (and nobody has written a Join)
     const int lane = static_cast<int>(threadIdx.x & 31), warp = static_cast<int>(threadIdx.x >> 5);
     const Join x = joins[blockIdx.x + 1];
     if (*reinterpret_cast<volatile unsigned int*>(&g_attnw_status) != 0u || x.parts == 0) return;

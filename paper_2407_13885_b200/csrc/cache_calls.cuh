@@ -225,7 +225,7 @@ PagedWorkspace paged_workspace(const attnw_cache* c, int tokens, int heads, bool
 
 template <int D>
 int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
-                 char* workspace, const PagedWorkspace& w, int tokens, int heads, float scale, int sm_count, cudaStream_t stream) {
+                 char* workspace, const PagedWorkspace& w, int tokens, int heads, float scale, int least, int sm_count, cudaStream_t stream) {
     using L = pa::Smem<D>;
     const int group = heads / c->kv_heads, tile_tokens = 128 / group;
     CUtensorMap tm_q, tm_k, tm_v;
@@ -237,34 +237,36 @@ int launch_paged(const attnw_cache* c, const void* Q, const long long* q_strides
     if (rc == ATTNW_OK) rc = encode_3d(&tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c->K, D, c->page, places, 64, box);
     if (rc == ATTNW_OK) rc = encode_3d(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c->V, D, c->page, places, 64, box);
     if (rc != ATTNW_OK) return rc;
-    if (allow_smem<pa::attn_paged_kernel<D>>(L::kDynamicBytes) != cudaSuccess) {
+    if ((least > 1 ? allow_smem<pa::attn_paged_kernel<D, true>>(L::kDynamicBytes) : allow_smem<pa::attn_paged_kernel<D, false>>(L::kDynamicBytes)) != cudaSuccess) {
         (void)cudaGetLastError();
         return ATTNW_ERR_CUDA;
     }
     const paged::Cache view = view_of(c);
     // As many CTAs as may have something to do: the most that all blocks can cost, by the shortest stretches.
-    const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(std::min(c->sequences, tokens))) * c->kv_heads;
+    const int sequences = std::min(c->sequences, tokens / least);  // at most, that have new tokens of ours
+    const long long blocks = (tokens / (2 * tile_tokens) + static_cast<long long>(sequences)) * c->kv_heads;
     const long long capacity = static_cast<long long>(c->table_width) * c->page, most = blocks * (pa::kBlockCost + capacity * (tokens > tile_tokens ? 2 : 1));
     const int ctas = static_cast<int>(std::min({static_cast<long long>(kPagedCtas), static_cast<long long>(sm_count), (most + pa::kLeastEven - 1) / pa::kLeastEven}));
-    const pa::Shape shape{tokens, heads, group, tile_tokens, w.part_rows, w.q_tiles, ctas};
+    const pa::Shape shape{tokens, heads, group, tile_tokens, w.part_rows, w.q_tiles, ctas, least};
     auto* stats = w.part_rows > 0 ? reinterpret_cast<float2*>(workspace + w.stats) : nullptr;
     auto* joins = w.part_rows > 0 ? reinterpret_cast<pa::Join*>(workspace + w.joins) : nullptr;
     auto* part = w.part_rows > 0 ? reinterpret_cast<float*>(workspace + w.o) : nullptr;
     const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
     auto* o = static_cast<__nv_bfloat16*>(O);
     auto* lse2 = mass ? reinterpret_cast<float*>(workspace + w.lse2) : nullptr;
-    cudaError_t e = launch_overlapped(pa::attn_paged_kernel<D>, static_cast<unsigned>(ctas), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
+    const auto kernel = least > 1 ? pa::attn_paged_kernel<D, true> : pa::attn_paged_kernel<D, false>;
+    cudaError_t e = launch_overlapped(kernel, static_cast<unsigned>(ctas), pa::kThreads, L::kDynamicBytes, stream, 1, tm_q, tm_k, tm_v, view,
                                       shape, starts, scale_log2e, o, lse, lse2, part, stats, joins);
     if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && part && ctas > 1) {
         const unsigned slices = static_cast<unsigned>((w.part_rows + pa::kJoinRows * pa::kJoinWarps - 1) / (pa::kJoinRows * pa::kJoinWarps));
-        e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, part, stats, joins, o,
+        e = launch_overlapped_3d(pa::combine_kernel<D>, static_cast<unsigned>(ctas - 1), slices, 1, pa::kJoinWarps * 32, stream, view, shape, starts, part, stats, joins, o,
                                  lse, lse2);
         if (e == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     if (e == cudaSuccess && mass) {
         // segments: at most kSegments more than one a (sequence with new tokens, key head)
-        const long long segments = pm::kSegments + static_cast<long long>(std::min(c->sequences, tokens)) * c->kv_heads;
+        const long long segments = pm::kSegments + static_cast<long long>(sequences) * c->kv_heads;
         e = allow_smem<pm::mass_kernel<D>>(pm::Smem<D>::kDynamicBytes);
         if (e == cudaSuccess)
             e = launch_overlapped(pm::mass_kernel<D>, static_cast<unsigned>(segments), pm::kThreads, pm::Smem<D>::kDynamicBytes, stream, 1, tm_q, tm_k, view, shape,
@@ -335,11 +337,11 @@ FewShape few_shape(DeviceInfo* dev, const attnw_cache* c, int tokens, int heads,
 
 template <int D, int GP, bool WEIGH>
 cudaError_t launch_few(const attnw_cache* c, const FewShape& f, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass,
-                       float* mass_out, int tokens, int heads, float scale, cudaStream_t stream) {
+                       float* mass_out, int tokens, int heads, float scale, int turns, cudaStream_t stream) {
     constexpr int most = few::Smem<D, GP>::bytes(few::kMaxScores / (GP + 1) / few::kUnit * few::kUnit, WEIGH);
     cudaError_t e = allow_smem<few::attn_few_kernel<D, GP, WEIGH>>(most);
     if (e != cudaSuccess) return e;
-    const few::Shape shape{tokens, heads, heads / c->kv_heads, f.cluster, f.max_keys};
+    const few::Shape shape{tokens, heads, heads / c->kv_heads, f.cluster, f.max_keys, turns};
     const float scale_log2e = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
     const long long items = static_cast<long long>(WEIGH ? c->sequences : tokens) * c->kv_heads;
     return launch_overlapped(few::attn_few_kernel<D, GP, WEIGH>, static_cast<unsigned>(items * f.cluster), few::kThreads,
@@ -350,12 +352,12 @@ cudaError_t launch_few(const attnw_cache* c, const FewShape& f, const void* Q, c
 
 template <int D, bool WEIGH>
 cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse,
-                             const float* mass, float* mass_out, int tokens, int heads, float scale, cudaStream_t stream) {
+                             const float* mass, float* mass_out, int tokens, int heads, float scale, int turns, cudaStream_t stream) {
     const auto launch = f.gp == 1   ? launch_few<D, 1, WEIGH>
                         : f.gp == 2 ? launch_few<D, 2, WEIGH>
                         : f.gp == 4 ? launch_few<D, 4, WEIGH>
                                     : launch_few<D, 8, WEIGH>;
-    return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, stream);
+    return launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, turns, stream);
 }
 
 // Is it the faster one?  Its time goes by the bytes that a CTA reads, 25 us a MB, more with many heads, and some 3 us a round of CTAs besides; the
@@ -366,12 +368,20 @@ cudaError_t launch_few_group(const attnw_cache* c, const FewShape& f, const void
 // 30 / 42.  With weights: 1 over 1000 9.9 / 32.6, 16000 31 / 47, 32 over 4095 134 / 223, 64 heads on 8, 8 over 4000 57 / 74; four tokens of one sequence
 // over 100 24.7 / 21.1.
 bool few_pays(const attnw_cache* c, const FewShape& f, int tokens, bool weigh) {
-    if (weigh && tokens > c->sequences) return false;  // (a sequence's tokens take turns there)
+    if (weigh && tokens > c->sequences) return false;  // (then some sequence has several, and those take turns there: kTurns)
     long long most = f.gp <= 4 ? 1024 : 512;  // kB
     if (weigh) most = f.gp <= 4 ? 16384 : 4096;
     if (tokens > c->sequences) most = most * 3 / 4;  // (the other one reads a sequence's keys once for all its tokens)
     return f.rounds * (f.max_keys * 4ll * c->d / 1024 + 128) <= most + 128;
 }
+
+// With weights the kernel for few tokens has one cluster a (sequence, key head), and several tokens of one sequence take turns in it, each of them a pass over its
+// keys.  How the new tokens are dealt out is on the device: as many as there are sequences may be one of each, or a chunk of one among others that are
+// idle.  So sequences with more than kTurns are left to the other kernels, which are launched behind it and at once find out if there are none; calls of up to
+// kTurnsInAll tokens are spared that.  us per call, 32 heads on 8, d = 128, alone -> with the others behind it: 64 sequences of 256 keys with one token each 36.4 ->
+// 40.7, 32 of 4096 134 -> 140, 256 of 256 130 -> 136, 16 of 256 9.7 -> 14.4 (spared); a chunk of 16, 32, 64 and 256 of one among as many of 256 keys 113 -> 29
+// (spared), 223 -> 25, 440 -> 33 and 1650 -> 76, of 32 among 32 of 4096 849 -> 46.  (The tensor cores for all: 65, 184, 342, 28 and 20, 23, 37, 165, 43.)
+constexpr int kTurns = 8, kTurnsInAll = 16;
 
 int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides, const int* starts, void* O, float* lse, const float* mass, float* mass_out,
                 void* workspace, unsigned long long workspace_bytes, int tokens, int heads, float scale, void* stream) {
@@ -408,20 +418,24 @@ int paged_entry(const attnw_cache* c, const void* Q, const long long* q_strides,
     const int variant = g_paged_variant.load(std::memory_order_relaxed);
     const FewShape f = variant == 1 ? FewShape{} : few_shape(dev, c, tokens, heads, mass != nullptr);
     if (variant == 2 && f.gp == 0) return ATTNW_ERR_UNSUPPORTED;
+    int least = 1;
     if (f.gp > 0 && (variant == 2 || few_pays(c, f, tokens, mass != nullptr))) {
+        const bool both = variant == 0 && mass && tokens > kTurnsInAll;
         const auto launch = c->d == 64 ? (mass ? launch_few_group<64, true> : launch_few_group<64, false>)
                                        : (mass ? launch_few_group<128, true> : launch_few_group<128, false>);
-        if (launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        if (launch(c, f, Q, q_strides, starts, O, lse, mass, mass_out, tokens, heads, scale, both ? kTurns : INT_MAX, static_cast<cudaStream_t>(stream)) !=
+            cudaSuccess) {
             (void)cudaGetLastError();
             return ATTNW_ERR_CUDA;
         }
         g_launches.fetch_add(1, std::memory_order_relaxed);
-        return ATTNW_OK;
+        if (!both) return ATTNW_OK;
+        least = kTurns + 1;
     }
     rc = load_encoder();
     if (rc != ATTNW_OK) return rc;
     const auto launch = c->d == 64 ? launch_paged<64> : launch_paged<128>;
-    return launch(c, Q, q_strides, starts, O, lse, mass, mass_out, static_cast<char*>(workspace), w, tokens, heads, scale, dev->sm_count,
+    return launch(c, Q, q_strides, starts, O, lse, mass, mass_out, static_cast<char*>(workspace), w, tokens, heads, scale, least, dev->sm_count,
                   static_cast<cudaStream_t>(stream));
 }
 

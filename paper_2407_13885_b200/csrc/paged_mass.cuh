@@ -129,6 +129,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
+    if (shape.least > 1 && pa::nothing_to_do(cache, shape, starts)) return;
 
     // ---- set-up ------------------------------------------------------------------------------
     if (warp == kProducer && lane == 0) {
@@ -297,6 +298,7 @@ mass_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const int rows = cache.sequences * cache.kv_heads;
             for (int r = static_cast<int>(blockIdx.x); r < rows && !failed; r += static_cast<int>(gridDim.x)) {
                 const pa::Share s = pa::share_of(cache, shape, starts, r / cache.kv_heads);
+                if (s.n == 0 && shape.least > 1) continue;  // (attn_few_kernel's)
                 for (int j = (s.n > 0 ? s.length : 0) + (warp - 8) * 32 + lane; j < capacity; j += 256)
                     mass_out[static_cast<size_t>(r) * capacity + j] = mass[static_cast<size_t>(r) * capacity + j];
             }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paged_reference import Paged
+from test_gpu_cache import check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -175,3 +176,64 @@ def test_a_score_of_minus_infinity_weighs_nothing(attnw, variant):
     got = attend(attnw, c, Q)
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+# ---- weights of keys where some sequences have many new tokens and others few ---------------------------------------------------
+
+DEALT_OUT = [  # (H, Hkv, d, page, pairs)
+    (8, 2, 64, 16, [(0, 200)] * 30 + [(25, 300)] + [(0, 70)] * 9),                       # a chunk of one among idle ones
+    (32, 8, 128, 64, [(0, 200)] * 60 + [(48, 48)] + [(0, 0), (0, 256), (0, 1)]),
+    (8, 2, 128, 16, [(1, 40 + 7 * i) for i in range(40)]),                                # one of each
+    (6, 3, 64, 32, [(8, 200), (0, 90), (9, 100), (1, 64), (0, 300), (17, 40)] + [(0, 100)] * 40),
+    (4, 4, 128, 32, [(9, 9), (8, 8), (16, 500), (1, 1), (0, 0), (30, 20)] + [(0, 33)] * 70),
+    (2, 1, 64, 16, [(1, 100)] * 20 + [(200, 1500)] + [(1, 90)] * 20 + [(0, 50)] * 250),
+]
+
+
+@pytest.mark.parametrize("H,Hkv,d,page,pairs", DEALT_OUT)
+@pytest.mark.parametrize("apart", [False, True])
+def test_weights_of_tokens_that_are_dealt_out_unevenly(attnw, H, Hkv, d, page, pairs, apart):
+    c = Paged(pairs, Hkv, d, page, seed=31, behind=2)
+    c.tokens = min(c.tokens, len(pairs))                 # as many tokens as sequences, at most: the rule's own condition
+    assert c.tokens > 16 and sum(n for n, _ in pairs) <= c.tokens
+    Q = c.normal(c.tokens, H, d)
+    for _ in range(2):                                   # (the second time with what the first left in the workspace)
+        check_attention(attnw, c, Q, d ** -0.5)
+    if not apart:
+        return
+    mass = torch.rand(len(pairs), Hkv, c.width * page, generator=c.gen).cuda()
+    before = attnw.launch_count()
+    O, out = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, d ** -0.5, mass=mass)   # mass_out is other memory
+    assert attnw.launch_count() - before >= 2            # not all by clusters that take one token after the other
+    same = mass.clone()
+    P, _ = attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, d ** -0.5, mass=same, mass_out=same)
+    assert torch.equal(O[:sum(n for n, _ in pairs)], P[:sum(n for n, _ in pairs)]) and torch.equal(out, same)
+    untouched = torch.arange(c.width * page, device="cuda")[None] >= c.lengths[:, None] * (c.starts.diff() > 0)[:, None]
+    assert torch.equal(out.masked_select(untouched[:, None]), mass.masked_select(untouched[:, None]))
+
+
+def test_a_captured_call_follows_the_starts(attnw):
+    # Captured with one token of each sequence, replayed with a chunk of one, and back.
+    c = Paged([(1, 300)] * 40, 2, 64, 16, seed=32)
+    Q, mass = c.normal(40, 8, 64), torch.rand(40, 2, c.width * 16, generator=c.gen).cuda()
+    call = lambda: attnw.attn_paged(Q, c.K, c.V, c.table, c.lengths, c.starts, 0.125, mass=mass)  # noqa: E731
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        got = call()
+    one = torch.arange(41, dtype=torch.int32, device="cuda")
+    chunk = torch.where(one <= 7, 0, 40).to(torch.int32)
+    for starts in (chunk, one, chunk, one):
+        c.starts.copy_(starts)
+        want = call()
+        for t in got:
+            t.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        c.pairs = [(int(n), 300) for n in starts.diff()]
+        check_attention(attnw, c, Q, 0.125)
