@@ -63,6 +63,67 @@ def test_eviction_of_keys_without_a_page(attnw, in_place, d):
     assert torch.equal(bits(c.K), bits(want_K)) and torch.equal(bits(c.V), bits(want_V))
 
 
+def kept_by_definition(row, length, budget, recent):
+    """The last `recent` keys, and of the others those of most weight: of equal ones the first, NaN below every number."""
+    if length <= budget:
+        return torch.arange(length)
+    old = row[:length - recent].double()
+    nan = torch.isnan(old)
+    by_weight = torch.argsort(old.masked_fill(nan, -math.inf), descending=True, stable=True)
+    order = by_weight[torch.argsort(nan[by_weight].to(torch.int8), stable=True)]
+    return torch.cat((order[:budget - recent].sort().values, torch.arange(length - recent, length)))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("budget,recent,lengths", [
+    (1000, 100, [16385 + 100, 16384 + 100, 16384 + 101]),   # keys to choose from: one more than the first turn has, and as many
+    (20000, 77, [40003, 20000, 20001, 33000]),
+    (33000, 0, [49153, 32768, 33001]),
+    (5, 5, [40000, 3]),
+    (16400, 16390, [36001]),
+])
+@pytest.mark.parametrize("weights", ["spread", "near", "ties", "equal", "odd", "late"])
+def test_eviction_of_long_rows(attnw, budget, recent, lengths, in_place, weights):
+    page, Hkv, d = 64, 2, 64
+    c = Paged([(0, n) for n in lengths], Hkv, d, page, seed=budget + recent, spare=1 + len(lengths) * -(-budget // page))
+    C = c.width * page
+    mass = torch.randn(len(lengths), Hkv, C, generator=c.gen).mul(2).exp()
+    if weights == "near":     # the same upper 13 bits for more keys than a list holds, and the same 24 for many
+        mass = 1.0 + torch.randint(0, 4096, mass.shape, generator=c.gen) * 2.0 ** -23
+    elif weights == "ties":   # equal to the last bit: the border lies among them, in the second or third turn
+        mass = (mass * 2).floor().clamp_max(3.0)
+    elif weights == "equal":
+        mass = torch.full_like(mass, 0.25)
+    elif weights == "late":   # the first keys have the least
+        mass = torch.where(torch.arange(C) < 15000, 0.125, 0.25).expand_as(mass).contiguous()
+    elif weights == "odd":
+        pool = torch.tensor([0.0, -0.0, math.inf, -math.inf, math.nan, 1e-45, -1.0, 3e38, 1.0])
+        mass = pool[torch.randint(0, 9, mass.shape, generator=c.gen)]
+    mass0, mass = mass, mass.cuda()
+    K0, V0 = c.K.cpu(), c.V.cpu()
+    width = c.width if in_place else -(-budget // page)
+    out = None if in_place else torch.tensor(c.spare[:len(lengths) * width], dtype=torch.int32, device="cuda").view(len(lengths), width)
+    kept, now, mass_out = attnw.cache_evict(c.K, c.V, c.table, c.lengths, mass, budget, recent, table_out=out, mass_out=mass if in_place else None)
+    assert now.tolist() == [min(n, budget) for n in lengths]
+    want_K, want_V = K0.clone(), V0.clone()
+    want_kept = torch.full((len(lengths), Hkv, budget), -1, dtype=torch.int32)
+    want_mass = torch.zeros(len(lengths), Hkv, width * page)
+    to_table = (c.table if in_place else out).cpu().long()
+    for b, length in enumerate(lengths):
+        for h in range(Hkv):
+            src = kept_by_definition(mass0[b, h], length, budget, recent)
+            t = torch.arange(len(src))
+            want_kept[b, h, :len(src)] = src.to(torch.int32)
+            want_mass[b, h, :len(src)] = mass0[b, h, src]
+            from_page, to_page = c.table[b].cpu().long()[src // page], to_table[b][t // page]
+            want_K[to_page, h, t % page], want_V[to_page, h, t % page] = K0[from_page, h, src % page], V0[from_page, h, src % page]
+    assert torch.equal(kept.cpu(), want_kept)
+    assert torch.equal(bits(mass_out), bits(want_mass))
+    assert torch.equal(bits(c.K), bits(want_K)) and torch.equal(bits(c.V), bits(want_V))
+    if not in_place:
+        assert torch.equal(bits(mass), bits(mass0))
+
+
 def test_a_budget_that_is_refused_takes_no_memory(attnw):
     c = Paged([(0, 100)] * 3, 2, 64, 16)
     mass = torch.rand(3, 2, c.width * 16, device="cuda")
