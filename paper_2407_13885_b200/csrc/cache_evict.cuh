@@ -290,13 +290,13 @@ evict_move_kernel(paged::Cache cache, const int* table_out, int table_out_width,
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int t = t0 + first + i * stride;
-            from[i] = t < left ? source_of(keep[t], t, length) : -1;
+            from[i] = t < left ? keep[t] : -1;
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int t = t0 + first + i * stride;
             to[i] = -1;
-            if (from[i] < 0 || (IN_PLACE && from[i] == t)) continue;
+            if (source_of(from[i], t, length) < 0 || (IN_PLACE && from[i] == t)) continue;
             const int page = paged::page_of(cache.table, cache, b, from[i]), page_to = target_page(t);
             if (page_to < 0) continue;
             to[i] = static_cast<long long>(paged::row_offset(cache, page_to, h, t) / 8 + piece);
