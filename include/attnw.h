@@ -194,6 +194,8 @@ int attnw_cache_append(const attnw_cache* cache, const void* Q, const void* K, c
  *   workspace    device, 16-byte aligned, at least attn_paged_workspace(cache, tokens, heads, mass != NULL) bytes, in use until the
  *                call's work has ended; it keeps nothing from one call to the next and may hold anything
  *   heads        a multiple of kv_heads, at most 128 to one;  scale finite, >= 0;  tokens * heads < 2^29
+ * Scores, sums and weights in mass are float32.  For the product with V the weights are rounded to bfloat16 by the kernel on the tensor cores (2^-8 of each);
+ * the kernel for few tokens keeps 16 bits of them, or 24 with one or two heads a key head (attnw_set_paged_variant).
  * Keys that a token does not see are never part of its result, whatever the cache holds there: those behind its own place, and those behind the sequence's
  * length.  A value that is not finite makes its feature of the tokens that see it, and of no others, not finite.  A score that is not a number makes its
  * row's O and lse, and the weights that it adds to, not a number.
@@ -227,6 +229,7 @@ int attnw_set_paged_variant(int variant);
  *   kept         device, int32, [sequences, kv_heads, budget]: the old place of each key that stays, -1 behind them
  *   lengths_out  device, int32, [sequences]: the new lengths; not cache->lengths
  *   budget       1 ... the places of the pages that take them;  recent 0 ... budget
+ * Afterwards a key's place no longer is its position: who turns the next tokens by their positions (attnw_cache_append) counts those apart from lengths.
  */
 int attnw_cache_evict(const attnw_cache* cache, const int* table_out, int table_out_width, const float* mass, float* mass_out, int* kept, int* lengths_out,
                       int budget, int recent, void* stream);

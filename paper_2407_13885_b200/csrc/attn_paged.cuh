@@ -16,9 +16,10 @@
 // begin and end inside a block: then its unnormalised O, offset and sum go to a workspace, and combine_kernel joins them.  A CTA
 // goes through its blocks without a stop: while its Softmax warps finish one, the tiles of the next arrive.
 //
-// Bound: HBM for single tokens over long caches (24 over up to 32768 keys, 32 heads on 8, d = 128, 1.8 GB: 283 us, 6.5 TB/s, as fast as a plain copy; 325 in
+// Bound: HBM for single tokens over long caches (24 over up to 32768 keys, 32 heads on 8, d = 128, 1.8 GB: 284 us, 6.5 TB/s, as fast as a plain copy; 332 in
 // a loop at the power cap).  For chunks tensor pipe and special function units, 1024 cycles each a tile of 128 x 128 at d = 128: 4 x 2048 tokens over some
-// 6000 keys each 690 us, 1.05 PFLOP/s (780 in a loop); the pipe is at 48 %, the rest are hand-overs between the roles and tiles cut by the diagonal.
+// 6000 keys each 705 us, 1.03 PFLOP/s (817 in a loop, 0.89); both at 55 % in one such sequence, 50 % in 2 x 1024 over 4000, the rest are hand-overs between
+// the roles and tiles cut by the diagonal.
 #pragma once
 #include <cstddef>
 
@@ -251,8 +252,9 @@ struct Walk {
         blocks = warp_sum(blocks);
         stretch = max(static_cast<long long>(kLeastCost), divided(total + s.ctas - 1, s.ctas));
         // Few blocks: a CTA's way from one to the next takes as long as several key tiles, so none has parts of two.  Rounded up to whole stretches
-        // they take at most a stretch more each.  (us per call, 32 heads on 8, d = 128, one token over 4000 keys, 8 blocks: 24.1 -> 20.0; not with more: 4
-        // tokens, 32 blocks, 28.0 -> 31.9.)
+        // they take at most a stretch more each.  (us per call without -> with it, d = 128, single tokens over 4000 keys: 8 blocks 19.3 -> 16.2, 16 20.3 -> 17.5,
+        // 24 21.2 -> 20.1, 32 22.9 -> 25.4; over 16000: 4 blocks 32.8 -> 37.0, 8 34.1 -> 32.3, 16 37.5 -> 36.9, 18 39.4 -> 39.6, 24 45.4 -> 45.9, 32 54 -> 56; over
+        // 2000, d = 64: 16 19.3 -> 17.3, 40 21.2 -> 20.6, 64 23.1 -> 26.1.  kFewBlocks is where the longest stop to gain.)
         even = !__any_sync(0xffffffffu, many) && blocks <= kFewBlocks && 2 * blocks <= s.ctas;
         if (even) stretch = max(static_cast<long long>(kLeastEven), divided(total + (s.ctas - blocks) - 1, s.ctas - blocks));
         const long long at = index * stretch;

@@ -12,9 +12,10 @@
 // a row are one CTA's; for enough CTAs the row's features are dealt out, down to 32 bytes (a sector of DRAM) each, since the features of a key
 // move alike.
 //
-// Bound by HBM where rows are many: 128 rows of up to 16384 keys of 128 features to 4096 in place 99 us, 16.7 of them evict_select, whose one CTA a row
-// works through its histogram, and 82 evict_move (4.8 TB/s: a step's reads end before its writes begin).  8 rows of 4096 to 2048: 13.0 us, two launches'
-// latency.
+// Bound by HBM where rows are many: 128 rows of up to 16384 keys of 128 features to 4096 take 100 us to other pages and 109 in place (the bytes 73), 17 of them
+// evict_select, whose one CTA a row works through its histogram, the others evict_move.  In place a step's reads end before its writes begin; to other pages
+// reads and writes of all CTAs mix, and what keeps them at 5.7 TB/s has not been found.  8 rows of 4096 to 2048: 13.1 us to other pages, 17.0 in place, two
+// launches' latency and one CTA a row.  More than 16384 keys a row: 32 rows of 40000 to 8000 87 and 113 us (the bytes 41).
 #pragma once
 #include <cstdint>
 

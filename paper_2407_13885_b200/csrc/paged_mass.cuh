@@ -7,8 +7,8 @@
 // some of their keys; where a sequence has one query tile (decoding) that one stays and the keys stream past it.
 //
 // Bound: one exponential an element, 1024 cycles of the special function units a tile of 128 x 128 against 512 of the tensor pipe; for single tokens the
-// keys' way from HBM.  Measured: 1024 new tokens of each of two sequences over 5000 keys, 32 heads on 8, d = 128: 165 us, the special function units at
-// 65 % while a CTA works; segments are whole key tiles, here five, where 4.3 would be one for each SM.
+// keys' way from HBM.  Measured: 1024 new tokens of each of two sequences over 5000 keys, 32 heads on 8, d = 128: 166 us, the special function units at
+// 60 % while a CTA works; segments are whole key tiles, here five, where 4.3 would be one for each SM.
 #pragma once
 #include <cstddef>
 #include <type_traits>
